@@ -1,6 +1,6 @@
 /*
  * tacg.h -- C ABI of the MI355X (gfx950) trace passes of Task-Aware Coactivation Grouping (TACG) and
- * Generic Expert Shared Replication (GESR).
+ * Generic Expert Shared Replication (GESR), and of the router and the experts' products around them.
  *
  * Conventions shared by every call
  *   - Pointers are DEVICE pointers unless the parameter name ends in `_host`.  The caller allocates
@@ -47,9 +47,24 @@ extern "C" {
 #define TACG_ERR_ID_DUP 0x2u   /* an expert id repeated within one token-layer           */
 #define TACG_ERR_TABLE 0x4u    /* placement / secondary entry >= G, or repeated in a set */
 #define TACG_ERR_LIMIT 0x8u    /* more than TACG_MAX_REPLICATED experts with secondaries  */
+#define TACG_ERR_VALUE 0x10u   /* a NaN or +inf logit; a weight (or its scale) that is not finite */
 
 /* flags */
 #define TACG_ACCUMULATE 0x1u /* tacg_coact_build: add into D and C instead of overwriting */
+
+/* element types of the router's and the experts' tensors */
+#define TACG_F32 0
+#define TACG_BF16 1
+#define TACG_F16 2
+
+/* scores of the router */
+#define TACG_SOFTMAX 0
+#define TACG_SIGMOID 1
+
+/* what tacg_expert_q4 makes of its products */
+#define TACG_Q4_EACH 0
+#define TACG_Q4_GLU 1
+#define TACG_Q4_SUM 2
 
 /* limits */
 #define TACG_MAX_EXPERTS 256
@@ -59,6 +74,7 @@ extern "C" {
 #define TACG_MAX_SECONDARY 4
 #define TACG_MAX_REPLICATED 16
 #define TACG_MAX_TOP_PAIRS 4096
+#define TACG_MAX_WIDTH 65536 /* rows and columns of an expert's 4-bit weights */
 #define TACG_NOALLOC_SCRATCH_BYTES ((size_t)32 << 20) /* device scratch of the no-allocation entry point */
 
 /*
@@ -287,6 +303,90 @@ int tacg_group_objective(const float* a_tilde, int32_t n_layers, int32_t n_exper
  */
 int tacg_jain(const uint32_t* load, int32_t n_place, int32_t n_layers, int32_t n_gpus, int32_t per_layer,
               float* jain, float* maxvio, void* hip_stream);
+
+/*
+ * The router: top-k experts and gates of every token from its logits, and, for training, per-expert counts and balance losses.
+ * Logits: type `dtype`, E contiguous values per row; the row of token t at layer l starts at element
+ * l * stride_layer + t * stride_token (strides >= 0; aligned to the element).  A logit of -inf makes its expert unavailable to that
+ * token; the type's lowest finite value does not.  Scores over the available experts:
+ *   TACG_SOFTMAX  s_e = exp(x_e - norm),  norm = log sum exp x     TACG_SIGMOID  s_e = 1 / (1 + exp(-x_e)),  norm = sum s
+ * Selection: the k available experts of largest logit (without bias; the order is that of the scores), or of largest s_e +
+ * bias[l][e] (finite; it takes part in the selection alone); ties go to the lower id.
+ *   trace[l][t][j] = the j-th of them, -1 where fewer than k are available;
+ *   gate[l][t][j]  = scale * s, or with `renormalise` scale * s / (sum of the selected s), 0 where that sum is 0 or the id -1.
+ * Balance outputs (D, tokens, balance together, or all NULL), over the T = tokens[f][l] rows of family f at layer l that have
+ * an available expert, with s' = s (softmax) or s / norm (sigmoid):
+ *   D[f][l][e]     = number of those rows whose selection contains e (as tacg_coact_build counts the trace)
+ *   balance[f][l]  = sum_e (E / (k T) D_e) (1/T sum_t s'_e(t))         z[f][l] = 1/T sum_t norm_t^2
+ * and 0 where T = 0.  z is optional and for TACG_SOFTMAX (else TACG_E_INVAL).  norm[L][N] is optional, 0 (sigmoid) or -inf
+ * (softmax) for a row without an available expert.  Scores and sums are held in 32 bits, sums over tokens in 64; results do not
+ * depend on the order of execution.  A trace with unused slots (-1) is not one that the trace passes above take.
+ * Outputs: int16 trace[L][N][k] (2-byte aligned), float gate[L][N][k], float norm[L][N], uint32 D[F][L][E], uint32 tokens[F][L],
+ * float balance[F][L], float z[F][L].  Data errors: TACG_ERR_VALUE (a NaN or +inf logit; that row counts as one without
+ * available experts).  workspace: tacg_route_workspace_bytes(...) bytes with the balance outputs, else may be NULL.
+ * scale is finite.
+ */
+int tacg_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+               int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+               int32_t score, const float* bias_or_null, int32_t renormalise, float scale, int16_t* trace, float* gate,
+               float* norm_or_null, uint32_t* D_or_null, uint32_t* tokens_or_null, float* balance_or_null,
+               float* z_or_null, uint32_t* d_err, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+size_t tacg_route_workspace_bytes(int64_t n_tokens, int32_t n_layers, int32_t n_experts, int32_t n_fam);
+
+/*
+ * Gradient of the router's gates and losses to its logits.  logits, trace, norm, D and tokens are those of tacg_route (selection
+ * and counts are constants, as usual for these losses); score, renormalise and scale too.
+ *   grad_logits = sum_{l,t,j} grad_gate d gate / d x  +  sum_{f,l} grad_balance d balance / d x  +  grad_z d z / d x
+ * in the type of the logits, contiguous [L][N][E].  grad_gate float [L][N][k] or NULL; grad_balance float [F][L] or NULL (else D and
+ * tokens are required); grad_z float [F][L] or NULL (TACG_SOFTMAX only; tokens required).  Unavailable experts and rows without
+ * any get 0.  Each value is held in 32 bits and rounded once.  Ids outside 0..E-1 are unused slots.
+ */
+int tacg_route_backward(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+                        int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+                        int32_t score, int32_t renormalise, float scale, const int16_t* trace, const float* norm,
+                        const uint32_t* D_or_null, const uint32_t* tokens_or_null, const float* grad_gate_or_null,
+                        const float* grad_balance_or_null, const float* grad_z_or_null, void* grad_logits,
+                        void* hip_stream);
+
+/*
+ * Weights in 4 bits with a scale (and a zero) per group of columns of a row.  Row r of a matrix of n_cols columns holds
+ *   q[r][ceil(n_cols / 32) * 16] bytes, column c in byte c / 2, the even one in the low four bits (levels past n_cols are not read);
+ *   scales[r][G], zeros[r][G] (uint8, 0..15; NULL: all 8) with G = ceil(n_cols / group), group 32, 64, 128 or 256;
+ *   W[r][c] = scales[r][c / group] * (level - zero).
+ * tacg_q4_pack makes them of W in `dtype`, rows `row_stride` elements apart, scales in `scale_dtype` (TACG_BF16 or TACG_F16):
+ *   without zeros  scale = max |W| / 7,  level = clamp(round(W / scale) + 8, 0, 15)
+ *   with zeros     lo = min(0, min W), hi = max(0, max W), scale = (hi - lo) / 15, zero = clamp(round(-lo / scale), 0, 15),
+ *                  level = clamp(round(W / scale) + zero, 0, 15)
+ * per group, with the scale as rounded to its type, in 32-bit arithmetic, halves to even; a group whose scale is 0 gets the
+ * level 8 (and zero 8).  Data errors: TACG_ERR_VALUE (a weight that is not finite, or a scale that its type cannot hold).
+ */
+int tacg_q4_pack(const void* w, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride, int32_t group,
+                 int32_t scale_dtype, uint8_t* q, void* scales, uint8_t* zeros_or_null, uint32_t* d_err,
+                 void* hip_stream);
+
+/*
+ * Products of tokens with the 4-bit weights of the experts that they are routed to, of those that this GPU holds.
+ * W holds n_held matrices of n_rows x n_cols one after the other (layout above; q 16-byte aligned, scales in `dtype`).  Slot j of
+ * token t is served by matrix h = slot_of_expert[ids[t][j]] (int32 [E]; NULL: h = id); an id of -1 or an h < 0 is served elsewhere.
+ * x(t, j) = the n_cols values from element t * stride_token + j * stride_slot of x (strides >= 0; 0 for one x per token).
+ *   TACG_Q4_EACH  out[t][j][n] = W_h[n] . x(t, j)                                                    (out [T][k][n_rows])
+ *   TACG_Q4_GLU   out[t][j][n] = silu(W_h[n] . x) * (W_h[n + n_rows / 2] . x)                        (out [T][k][n_rows / 2])
+ *   TACG_Q4_SUM   out[t][n]    = sum over served j, in slot order, of gate[t][j] * (W_h[n] . x(t, j))  (out [T][n_rows])
+ * with 0 for what is served elsewhere.  x, scales and out have type `dtype` (TACG_BF16 or TACG_F16), gate is float [T][k] (required for
+ * TACG_Q4_SUM).  Products are exact in the levels, sums are held in 32 bits, and the result is rounded once; it does not depend on
+ * the order of execution.  Data errors: TACG_ERR_ID_RANGE (id >= E or < -1), TACG_ERR_TABLE (h >= n_held); such slots are
+ * taken as served elsewhere.  workspace: tacg_expert_q4_workspace_bytes(...) bytes (NULL where that is 0).
+ * n_rows, n_cols <= TACG_MAX_WIDTH; T * k < 2^31.
+ */
+int tacg_expert_q4(const void* x, int32_t dtype, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
+                   int32_t top_k, int32_t n_experts, const int16_t* ids, const int32_t* slot_of_expert_or_null,
+                   int32_t n_held, const uint8_t* q, const void* scales, const uint8_t* zeros_or_null, int32_t group,
+                   int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate_or_null, void* out, uint32_t* d_err,
+                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+size_t tacg_expert_q4_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_rows,
+                                      int32_t n_cols, int32_t mode);
 
 /* Human-readable text of a status code (static storage). */
 const char* tacg_strerror(int status);

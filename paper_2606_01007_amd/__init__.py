@@ -12,6 +12,11 @@ kernels.  There is no fallback: if the library or the GPU is missing, the calls 
                           secondary, load_ref, theta=(3, 20))
     jain, maxvio = jain_index(out["load"])
 
+    r = route(logits, top_k, fam_off, balance=True)          # trace, gates, counts and balance losses of router logits
+    grad = route_backward(logits, r["trace"], r["norm"], fam_off, D=r["D"], tokens=r["tokens"], grad_balance=g)
+    q, scales, zeros = q4_pack(weights, group=128)           # experts in 4 bits
+    h = expert_q4(x, trace[l], q, scales, group=128, mode="glu")
+
 Unsigned 32-bit device outputs are held in torch.int32 tensors (same bits) and unsigned 64-bit ones in
 torch.int64 tensors; `as_u32` converts the former to int64 values.
 """
@@ -31,9 +36,12 @@ LIB_PATH = os.environ.get("TACG_LIBRARY") or os.path.join(_PKG, "libtacg.so")
 
 OK, E_INVAL, E_UNSUPPORTED, E_DEVICE, E_SCRATCH = 0, -1, -2, -3, -4
 NOALLOC_SCRATCH_BYTES = 32 << 20
-ERR_ID_RANGE, ERR_ID_DUP, ERR_TABLE, ERR_LIMIT = 0x1, 0x2, 0x4, 0x8
+ERR_ID_RANGE, ERR_ID_DUP, ERR_TABLE, ERR_LIMIT, ERR_VALUE = 0x1, 0x2, 0x4, 0x8, 0x10
 ACCUMULATE = 0x1
 NONE = 0xFF
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+SCORES = {"softmax": 0, "sigmoid": 1}
+Q4_MODES = {"each": 0, "glu": 1, "sum": 2}
 
 _lock = threading.Lock()
 _lib = None
@@ -81,6 +89,18 @@ def lib():
             L.tacg_gesr_scores.argtypes = [P, P, i32, i32, i32, i32, P, P, P, P]
             L.tacg_group_objective.argtypes = [P, i32, i32, P, i32, i32, P, P, P]
             L.tacg_jain.argtypes = [P, i32, i32, i32, i32, P, P, P]
+            f32 = ctypes.c_float
+            L.tacg_route.argtypes = [P, i32, i64, i64, i64, i32, i32, i32, P, i32, i32, P, i32, f32, P, P, P, P, P, P, P,
+                                     P, P, sz, P]
+            L.tacg_route_workspace_bytes.argtypes = [i64, i32, i32, i32]
+            L.tacg_route_workspace_bytes.restype = sz
+            L.tacg_route_backward.argtypes = [P, i32, i64, i64, i64, i32, i32, i32, P, i32, i32, i32, f32, P, P, P, P, P,
+                                              P, P, P, P]
+            L.tacg_q4_pack.argtypes = [P, i32, i64, i32, i64, i32, i32, P, P, P, P, P]
+            L.tacg_expert_q4.argtypes = [P, i32, i64, i64, i64, i32, i32, P, P, i32, P, P, P, i32, i32, i32, i32, P, P,
+                                         P, P, sz, P]
+            L.tacg_expert_q4_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+            L.tacg_expert_q4_workspace_bytes.restype = sz
             L.tacg_strerror.argtypes = [ctypes.c_int]
             L.tacg_strerror.restype = ctypes.c_char_p
             for name in ("tacg_coact_build", "tacg_reweight", "tacg_placement_load", "tacg_eval_placements",
@@ -453,3 +473,187 @@ def jain_index(load: torch.Tensor, per_layer: bool = False, stream=None):
                          _dptr(v), _stream(stream))
     _check("tacg_jain", st)
     return j, v
+
+
+# ---- the router and the experts' products --------------------------------------------------------
+
+def _logits(x: torch.Tensor):
+    """Pointer, type code and strides of router logits [L][N][E] whose rows are contiguous."""
+    if x.dim() != 3 or x.dtype not in DTYPES:
+        raise ValueError(f"logits: expected float32, bfloat16 or float16 [L][N][E], got {x.dtype} {tuple(x.shape)}")
+    if not x.is_cuda:
+        raise ValueError("expected a device tensor")
+    if x.stride(2) != 1 and x.shape[2] > 1:
+        raise ValueError("logits: the values of a row must be contiguous")
+    return x.data_ptr(), DTYPES[x.dtype], x.stride(0), x.stride(1)
+
+
+def _segments(fam_off, N: int) -> np.ndarray:
+    return np.array([0, N], dtype=np.int64) if fam_off is None else _fam_off(fam_off)
+
+
+def _score(score: str) -> int:
+    if score not in SCORES:
+        raise ValueError(f"score: expected one of {sorted(SCORES)}, got {score!r}")
+    return SCORES[score]
+
+
+def route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = "softmax", bias: Optional[torch.Tensor] = None,
+          renorm: bool = False, scale: float = 1.0, balance: bool = False, want_norm: bool = False,
+          ws: Optional[torch.Tensor] = None, err: Optional[torch.Tensor] = None, out: Optional[dict] = None,
+          stream=None) -> dict:
+    """Top-k experts and gates of router logits [L][N][E] (tacg_route).  fam_off: None = one family of all tokens.
+
+    dict(trace int16 [L][N][k], gate float32 [L][N][k], err), with want_norm or balance also norm float32 [L][N], and with
+    balance D [F][L][E], tokens [F][L] (uint32 bits), balance float32 [F][L] and, for softmax scores, z float32 [F][L].
+    Masked experts have the logit -inf; where fewer than k are left the trace holds -1 and the gate 0."""
+    if stream is not None:  # all of the call, its buffers too, on that stream
+        with torch.cuda.stream(stream):
+            return route(logits, top_k, fam_off, score, bias, renorm, scale, balance, want_norm, ws, err, out)
+    ptr, dtype, s_layer, s_token = _logits(logits)
+    L_, N, E = logits.shape
+    dev = logits.device
+    off = _segments(fam_off, N)
+    F = off.size - 1
+    code = _score(score)
+    if out is None:
+        out = dict(trace=torch.empty((L_, N, top_k), dtype=torch.int16, device=dev),
+                   gate=torch.empty((L_, N, top_k), dtype=torch.float32, device=dev))
+        if balance or want_norm:
+            out["norm"] = torch.empty((L_, N), dtype=torch.float32, device=dev)
+        if balance:
+            out.update(D=torch.empty((F, L_, E), dtype=torch.int32, device=dev),
+                       tokens=torch.empty((F, L_), dtype=torch.int32, device=dev),
+                       balance=torch.empty((F, L_), dtype=torch.float32, device=dev))
+            if code == 0:
+                out["z"] = torch.empty((F, L_), dtype=torch.float32, device=dev)
+    else:
+        out = dict(out)
+    get = out.get if balance else lambda name: None
+    if balance:
+        need = lib().tacg_route_workspace_bytes(N, L_, E, F)
+        if ws is None or ws.numel() < need:
+            ws = workspace(need, dev)
+    if err is None:
+        err = _err_tensor(dev)
+    st = lib().tacg_route(
+        ptr, dtype, s_layer, s_token, N, L_, top_k, E, _hptr(off), F, code,
+        _arg(bias, "bias", torch.float32, (L_, E)), 1 if renorm else 0, float(scale),
+        _arg(out["trace"], "trace", torch.int16, (L_, N, top_k)), _arg(out["gate"], "gate", torch.float32, (L_, N, top_k)),
+        _arg(out.get("norm"), "norm", torch.float32, (L_, N)), _arg(get("D"), "D", torch.int32, (F, L_, E)),
+        _arg(get("tokens"), "tokens", torch.int32, (F, L_)), _arg(get("balance"), "balance", torch.float32, (F, L_)),
+        _arg(get("z"), "z", torch.float32, (F, L_)), _arg(err, "err", torch.int32, (1,)),
+        _dptr(ws) if balance else None, ws.numel() if balance else 0, _stream())
+    _check("tacg_route", st)
+    out["err"] = err
+    return out
+
+
+def route_backward(logits: torch.Tensor, trace: torch.Tensor, norm: torch.Tensor, fam_off=None,
+                   D: Optional[torch.Tensor] = None, tokens: Optional[torch.Tensor] = None,
+                   grad_gate: Optional[torch.Tensor] = None, grad_balance: Optional[torch.Tensor] = None,
+                   grad_z: Optional[torch.Tensor] = None, score: str = "softmax", renorm: bool = False,
+                   scale: float = 1.0, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of gates and losses to the logits, [L][N][E] in their type (tacg_route_backward).  trace, norm, D and tokens are
+    those of `route` on the same logits with the same score, renorm and scale."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return route_backward(logits, trace, norm, fam_off, D, tokens, grad_gate, grad_balance, grad_z, score, renorm,
+                                  scale, out)
+    ptr, dtype, s_layer, s_token = _logits(logits)
+    L_, N, E = logits.shape
+    k = _trace_dims(trace)[2]
+    off = _segments(fam_off, N)
+    F = off.size - 1
+    if out is None:
+        out = torch.empty((L_, N, E), dtype=logits.dtype, device=logits.device)
+    st = lib().tacg_route_backward(
+        ptr, dtype, s_layer, s_token, N, L_, k, E, _hptr(off), F, _score(score), 1 if renorm else 0, float(scale),
+        _arg(trace, "trace", torch.int16, (L_, N, k)), _arg(norm, "norm", torch.float32, (L_, N)),
+        _arg(D, "D", torch.int32, (F, L_, E)), _arg(tokens, "tokens", torch.int32, (F, L_)),
+        _arg(grad_gate, "grad_gate", torch.float32, (L_, N, k)),
+        _arg(grad_balance, "grad_balance", torch.float32, (F, L_)), _arg(grad_z, "grad_z", torch.float32, (F, L_)),
+        _arg(out, "out", logits.dtype, (L_, N, E)), _stream())
+    _check("tacg_route_backward", st)
+    return out
+
+
+def q4_pack(weight: torch.Tensor, group: int = 128, symmetric: bool = True, scale_dtype: Optional[torch.dtype] = None,
+            err: Optional[torch.Tensor] = None, stream=None):
+    """Weights [H][N][K] in 4 bits (tacg_q4_pack): q uint8 [H][N][ceil(K / 32) * 16], scales [H][N][ceil(K / group)] in
+    scale_dtype (default: the weights' type, bfloat16 for float32 ones) and zeros (uint8, as scales) or None."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return q4_pack(weight, group, symmetric, scale_dtype, err)
+    if weight.dim() != 3 or weight.dtype not in DTYPES or not weight.is_cuda or not weight.is_contiguous():
+        raise ValueError(f"weight: expected a contiguous float device tensor [H][N][K], got {weight.dtype} "
+                         f"{tuple(weight.shape)}")
+    H, N, K = weight.shape
+    dev = weight.device
+    if scale_dtype is None:
+        scale_dtype = torch.bfloat16 if weight.dtype == torch.float32 else weight.dtype
+    if scale_dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"scale_dtype: expected bfloat16 or float16, got {scale_dtype}")
+    if group < 1:
+        raise ValueError(f"group: expected a positive number of columns, got {group}")
+    G = -(-K // group)
+    q = torch.empty((H, N, -(-K // 32) * 16), dtype=torch.uint8, device=dev)
+    scales = torch.empty((H, N, G), dtype=scale_dtype, device=dev)
+    zeros = None if symmetric else torch.empty((H, N, G), dtype=torch.uint8, device=dev)
+    if err is None:
+        err = _err_tensor(dev)
+    st = lib().tacg_q4_pack(weight.data_ptr(), DTYPES[weight.dtype], H * N, K, K, group, DTYPES[scale_dtype], _dptr(q),
+                            _dptr(scales), _dptr(zeros), _arg(err, "err", torch.int32, (1,)), _stream())
+    _check("tacg_q4_pack", st)
+    return q, scales, zeros
+
+
+def expert_q4(x: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, scales: torch.Tensor,
+              zeros: Optional[torch.Tensor] = None, group: int = 128, mode: str = "each",
+              n_experts: Optional[int] = None, slot_of_expert: Optional[torch.Tensor] = None,
+              gate: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, err: Optional[torch.Tensor] = None,
+              out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Products of tokens with the 4-bit weights of their experts (tacg_expert_q4).
+
+    x [T][K], or [T][k][K] where every slot has its own; rows contiguous, in bfloat16 or float16 as scales.  ids int16 [T][k]: the
+    routed experts (a layer of a trace).  q, scales, zeros: the n_held experts of this GPU (q4_pack); slot_of_expert int32 [E] gives
+    each expert's place among them, below 0 for an expert held elsewhere (None: all are held, in order).  mode: "each" -> [T][k][N],
+    "glu" -> [T][k][N / 2], "sum" (needs gate float32 [T][k]) -> [T][N].  Slots that are not served here add 0."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return expert_q4(x, ids, q, scales, zeros, group, mode, n_experts, slot_of_expert, gate, ws, err, out)
+    if ids.dim() != 2 or ids.dtype != torch.int16:
+        raise ValueError(f"ids: expected int16 [T][k], got {ids.dtype} {tuple(ids.shape)}")
+    if mode not in Q4_MODES:
+        raise ValueError(f"mode: expected one of {sorted(Q4_MODES)}, got {mode!r}")
+    if x.dtype not in (torch.bfloat16, torch.float16) or not x.is_cuda:
+        raise ValueError(f"x: expected a bfloat16 or float16 device tensor, got {x.dtype}")
+    T, k = ids.shape
+    K = x.shape[-1]
+    if tuple(x.shape) not in ((T, K), (T, k, K)):
+        raise ValueError(f"x: expected [{T}][K] or [{T}][{k}][K], got {tuple(x.shape)}")
+    if x.stride(-1) != 1 and K > 1:
+        raise ValueError("x: the values of a row must be contiguous")
+    if q.dim() != 3 or group < 1:
+        raise ValueError(f"q: expected [H][N][bytes] and a positive group, got {tuple(q.shape)}, {group}")
+    H, N = q.shape[:2]
+    E = H if n_experts is None else int(n_experts)
+    width = (H, N, -(-K // group))
+    if out is None:
+        shape = {"each": (T, k, N), "glu": (T, k, N // 2), "sum": (T, N)}[mode]
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    code = Q4_MODES[mode]
+    need = lib().tacg_expert_q4_workspace_bytes(T, k, E, N, K, code)
+    if need and (ws is None or ws.numel() < need):
+        ws = workspace(need, x.device)
+    if err is None:
+        err = _err_tensor(x.device)
+    st = lib().tacg_expert_q4(
+        x.data_ptr(), DTYPES[x.dtype], x.stride(0), x.stride(1) if x.dim() == 3 else 0, T, k, E, _dptr(ids),
+        _arg(slot_of_expert, "slot_of_expert", torch.int32, (E,)), H,
+        _arg(q, "q", torch.uint8, (H, N, -(-K // 32) * 16)), _arg(scales, "scales", x.dtype, width),
+        _arg(zeros, "zeros", torch.uint8, width), group, N, K, code, _arg(gate, "gate", torch.float32, (T, k)),
+        _arg(out, "out", x.dtype, {0: (T, k, N), 1: (T, k, N // 2), 2: (T, N)}[code]),
+        _arg(err, "err", torch.int32, (1,)), _dptr(ws), ws.numel() if ws is not None else 0, _stream())
+    _check("tacg_expert_q4", st)
+    return out

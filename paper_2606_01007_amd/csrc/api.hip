@@ -1,5 +1,6 @@
 // C ABI of libtacg: host-side argument validation, then enqueue on the caller's stream.
 // Argument errors return before any HIP call, so they can be exercised on a machine without a GPU.
+#include <cmath>
 #include <cstdint>
 #include <mutex>
 
@@ -23,6 +24,8 @@ int check_trace(const int16_t* trace, int64_t n_tokens, int32_t n_layers, int32_
     if (fam_off_host[f + 1] < fam_off_host[f]) return TACG_E_INVAL;
   return TACG_OK;
 }
+
+constexpr int64_t kNoTokens[2] = {0, 0};  // for the checks of sizes alone
 
 hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
 
@@ -329,6 +332,120 @@ int tacg_jain(const uint32_t* load, int32_t n_place, int32_t n_layers, int32_t n
   if (n_gpus > TACG_MAX_GPUS) return TACG_E_UNSUPPORTED;
   if (n_place == 0) return TACG_OK;
   return tacg::launch_jain(load, n_place, n_layers, n_gpus, per_layer, jain, maxvio, as_stream(hip_stream));
+}
+
+// Checks shared by the router's entry points: shapes, limits, strides and the family offsets.
+static int check_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+                       int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+                       int32_t score, int32_t renormalise, float scale) {
+  const int rc = check_trace(nullptr, 0, n_layers, top_k, n_experts, kNoTokens, 1);
+  if (rc != TACG_OK) return rc;
+  if (n_tokens < 0 || n_fam < 1 || fam_off_host == nullptr) return TACG_E_INVAL;
+  if (n_fam > TACG_MAX_FAMILIES || n_layers > 65535) return TACG_E_UNSUPPORTED;
+  if (n_tokens >= (int64_t(1) << 32) / top_k) return TACG_E_UNSUPPORTED;
+  if (fam_off_host[0] != 0 || fam_off_host[n_fam] != n_tokens) return TACG_E_INVAL;
+  for (int f = 0; f < n_fam; ++f)
+    if (fam_off_host[f + 1] < fam_off_host[f]) return TACG_E_INVAL;
+  if (dtype != TACG_F32 && dtype != TACG_BF16 && dtype != TACG_F16) return TACG_E_INVAL;
+  if (score != TACG_SOFTMAX && score != TACG_SIGMOID) return TACG_E_INVAL;
+  if ((renormalise != 0 && renormalise != 1) || !std::isfinite(scale)) return TACG_E_INVAL;
+  if (stride_layer < 0 || stride_token < 0) return TACG_E_INVAL;
+  if (n_tokens > 0 && (logits == nullptr || !aligned(logits, dtype == TACG_F32 ? 4 : 2))) return TACG_E_INVAL;
+  return TACG_OK;
+}
+
+size_t tacg_route_workspace_bytes(int64_t n_tokens, int32_t n_layers, int32_t n_experts, int32_t n_fam) {
+  if (n_tokens < 0 || n_layers < 1 || n_experts < 1 || n_fam < 1) return 0;
+  return tacg::route_workspace(n_tokens, n_layers, n_experts, n_fam);
+}
+
+int tacg_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+               int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+               int32_t score, const float* bias_or_null, int32_t renormalise, float scale, int16_t* trace, float* gate,
+               float* norm_or_null, uint32_t* D_or_null, uint32_t* tokens_or_null, float* balance_or_null,
+               float* z_or_null, uint32_t* d_err, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const int rc = check_route(logits, dtype, stride_layer, stride_token, n_tokens, n_layers, top_k, n_experts,
+                             fam_off_host, n_fam, score, renormalise, scale);
+  if (rc != TACG_OK) return rc;
+  if (d_err == nullptr || (n_tokens > 0 && (trace == nullptr || gate == nullptr))) return TACG_E_INVAL;
+  const bool bal = D_or_null != nullptr;
+  if (bal != (tokens_or_null != nullptr) || bal != (balance_or_null != nullptr)) return TACG_E_INVAL;
+  if (z_or_null != nullptr && (!bal || score != TACG_SOFTMAX)) return TACG_E_INVAL;
+  if (bal) {
+    const size_t need = tacg_route_workspace_bytes(n_tokens, n_layers, n_experts, n_fam);
+    if (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 256)) return TACG_E_INVAL;
+  }
+  return tacg::launch_route(logits, dtype, stride_layer, stride_token, n_tokens, n_layers, top_k, n_experts,
+                            fam_off_host, n_fam, score, bias_or_null, renormalise != 0, scale, trace, gate, norm_or_null,
+                            D_or_null, tokens_or_null, balance_or_null, z_or_null, d_err, workspace,
+                            as_stream(hip_stream));
+}
+
+int tacg_route_backward(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+                        int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+                        int32_t score, int32_t renormalise, float scale, const int16_t* trace, const float* norm,
+                        const uint32_t* D_or_null, const uint32_t* tokens_or_null, const float* grad_gate_or_null,
+                        const float* grad_balance_or_null, const float* grad_z_or_null, void* grad_logits,
+                        void* hip_stream) {
+  const int rc = check_route(logits, dtype, stride_layer, stride_token, n_tokens, n_layers, top_k, n_experts,
+                             fam_off_host, n_fam, score, renormalise, scale);
+  if (rc != TACG_OK) return rc;
+  if (grad_balance_or_null != nullptr && (D_or_null == nullptr || tokens_or_null == nullptr)) return TACG_E_INVAL;
+  if (grad_z_or_null != nullptr && (tokens_or_null == nullptr || score != TACG_SOFTMAX)) return TACG_E_INVAL;
+  if (n_tokens == 0) return TACG_OK;
+  if (norm == nullptr || grad_logits == nullptr || !aligned(grad_logits, dtype == TACG_F32 ? 4 : 2)) return TACG_E_INVAL;
+  if (grad_gate_or_null != nullptr && trace == nullptr) return TACG_E_INVAL;
+  return tacg::launch_route_backward(logits, dtype, stride_layer, stride_token, n_tokens, n_layers, top_k, n_experts,
+                                     fam_off_host, n_fam, score, renormalise != 0, scale, trace, norm, D_or_null,
+                                     tokens_or_null, grad_gate_or_null, grad_balance_or_null, grad_z_or_null, grad_logits,
+                                     as_stream(hip_stream));
+}
+
+static bool is_half(int32_t dtype) { return dtype == TACG_BF16 || dtype == TACG_F16; }
+static bool is_group(int32_t group) { return group == 32 || group == 64 || group == 128 || group == 256; }
+
+int tacg_q4_pack(const void* w, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride, int32_t group,
+                 int32_t scale_dtype, uint8_t* q, void* scales, uint8_t* zeros_or_null, uint32_t* d_err,
+                 void* hip_stream) {
+  if (dtype != TACG_F32 && !is_half(dtype)) return TACG_E_INVAL;
+  if (!is_half(scale_dtype) || n_rows < 0 || n_cols < 1 || row_stride < 0 || d_err == nullptr) return TACG_E_INVAL;
+  if (!is_group(group) || n_cols > TACG_MAX_WIDTH || n_rows > (int64_t(1) << 26)) return TACG_E_UNSUPPORTED;
+  if (n_rows == 0) return TACG_OK;
+  if (w == nullptr || !aligned(w, dtype == TACG_F32 ? 4 : 2) || q == nullptr || !aligned(q, 16)) return TACG_E_INVAL;
+  if (scales == nullptr || !aligned(scales, 2)) return TACG_E_INVAL;
+  return tacg::launch_q4_pack(w, dtype, n_rows, n_cols, row_stride, group, scale_dtype, q, scales, zeros_or_null, d_err,
+                              as_stream(hip_stream));
+}
+
+size_t tacg_expert_q4_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_rows,
+                                      int32_t n_cols, int32_t mode) {
+  if (n_tokens < 0 || top_k < 1 || n_experts < 1 || n_rows < 1 || n_cols < 1) return 0;
+  return tacg::expert_q4_workspace(n_tokens, top_k, n_experts, n_rows, n_cols, mode);
+}
+
+int tacg_expert_q4(const void* x, int32_t dtype, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
+                   int32_t top_k, int32_t n_experts, const int16_t* ids, const int32_t* slot_of_expert_or_null,
+                   int32_t n_held, const uint8_t* q, const void* scales, const uint8_t* zeros_or_null, int32_t group,
+                   int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate_or_null, void* out, uint32_t* d_err,
+                   void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const int rc = check_trace(nullptr, 0, 1, top_k, n_experts, kNoTokens, 1);
+  if (rc != TACG_OK) return rc;
+  if (!is_half(dtype) || n_tokens < 0 || n_held < 0 || n_rows < 1 || n_cols < 1 || d_err == nullptr) return TACG_E_INVAL;
+  if (stride_token < 0 || stride_slot < 0) return TACG_E_INVAL;
+  if (mode != TACG_Q4_EACH && mode != TACG_Q4_GLU && mode != TACG_Q4_SUM) return TACG_E_INVAL;
+  if (mode == TACG_Q4_GLU && n_rows % 2 != 0) return TACG_E_INVAL;
+  if (mode == TACG_Q4_SUM && gate_or_null == nullptr && n_tokens > 0) return TACG_E_INVAL;
+  if (!is_group(group) || n_rows > TACG_MAX_WIDTH || n_cols > TACG_MAX_WIDTH || n_held > TACG_MAX_EXPERTS)
+    return TACG_E_UNSUPPORTED;
+  if (n_tokens * static_cast<int64_t>(top_k) >= (int64_t(1) << 31)) return TACG_E_UNSUPPORTED;
+  if (n_held > 0 && (q == nullptr || scales == nullptr || !aligned(q, 16) || !aligned(scales, 2))) return TACG_E_INVAL;
+  if (n_tokens == 0) return TACG_OK;
+  if (x == nullptr || !aligned(x, 2) || ids == nullptr || out == nullptr || !aligned(out, 2)) return TACG_E_INVAL;
+  const size_t need = tacg_expert_q4_workspace_bytes(n_tokens, top_k, n_experts, n_rows, n_cols, mode);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 256))) return TACG_E_INVAL;
+  return tacg::launch_expert_q4(x, dtype, stride_token, stride_slot, n_tokens, top_k, n_experts, ids,
+                                slot_of_expert_or_null, n_held, q, scales, zeros_or_null, group, n_rows, n_cols, mode,
+                                gate_or_null, out, d_err, workspace, as_stream(hip_stream));
 }
 
 const char* tacg_strerror(int status) {

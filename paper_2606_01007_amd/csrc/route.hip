@@ -1,0 +1,700 @@
+// The router of a mixture-of-experts layer: top-k experts and gates from logits, per-expert counts and the balance and z losses
+// of every (family, layer) segment, and the gradient of gates and losses to the logits.
+//
+// A row is the E logits of one token at one layer.  Eight lanes share a row, so a wave holds eight rows; lane i of a row owns
+// the 16-byte chunks i, i + 8, i + 16, ... of it, as 32-bit floats in registers.  With s the scores (softmax, or sigmoid) and
+// s' = s (softmax) or s / sum s (sigmoid), a segment of T rows with D_e selections and M_e = sum_t s'_e(t) has
+//   balance = E / (k T^2) sum_e D_e M_e,   z = 1/T sum_t lse_t^2.
+//
+// route_main: one pass over the logits.  A workgroup takes a run of rows of one segment; its sums of s' (32 bits over a run, then 64),
+//   counts, rows and squares go to a slot of the workspace, and route_reduce adds a segment's slots in order in 64 bits, so
+//   that results do not depend on the order of execution.
+// route_back: one pass over logits and gradient; with c = d loss / d s' (a constant of the
+//   segment) and u the gradient of the scores through the gates, softmax: dx = s (c + u - sum s (c + u) + 2 gz lse / T).
+//   u has k entries a row: they are laid into a row of LDS, where each lane reads its own experts' back.
+#include <algorithm>
+#include <cmath>
+
+#include "tacg_internal.h"
+
+namespace tacg {
+namespace {
+
+constexpr int kRowLanes = 8;                     // lanes that share a row
+constexpr int kRouteThreads = 256;
+constexpr int kRouteWaves = kRouteThreads / 64;
+constexpr int kRowsPerPass = kRouteThreads / kRowLanes;
+constexpr float kNone = -INFINITY;
+
+struct RouteArgs {
+  const void* logits;
+  int64_t stride_layer, stride_token;            // elements
+  int64_t n_tokens;
+  int32_t n_layers, E, k, F, rows;               // rows: of a workgroup's run
+  int32_t softmax, renorm, vec;                  // vec: bytes that a load may take at a time
+  float scale;
+  const float* bias;                             // [L][E] or null
+  int16_t* trace;
+  float* gate;
+  float* norm;                                   // [L][N] or null
+  float* mass;                                   // workspace: [slots][E]
+  uint32_t* count;                               // [slots][E]
+  double* squares;                               // [slots]
+  uint32_t* routed;                              // [slots]
+  uint32_t* err;
+  int32_t run_off[TACG_MAX_FAMILIES + 1];        // first run of each family
+  int64_t fam_off[TACG_MAX_FAMILIES + 1];
+};
+
+struct BackArgs {
+  const void* logits;
+  int64_t stride_layer, stride_token;
+  int64_t n_tokens;
+  int32_t n_layers, E, k, F, rows, softmax, renorm, vec;
+  float scale;
+  const int16_t* trace;
+  const float* norm;
+  const uint32_t* D;                             // [F][L][E] or null
+  const uint32_t* tokens;                        // [F][L] or null
+  const float* grad_gate;                        // [L][N][k] or null
+  const float* grad_balance;                     // [F][L] or null
+  const float* grad_z;                           // [F][L] or null
+  void* grad;                                    // [L][N][E]
+  int32_t run_off[TACG_MAX_FAMILIES + 1];
+  int64_t fam_off[TACG_MAX_FAMILIES + 1];
+};
+
+struct Bf16 { uint16_t bits; };
+struct F16 { uint16_t bits; };
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(Bf16 x) { return __uint_as_float(static_cast<uint32_t>(x.bits) << 16); }
+__device__ __forceinline__ float widen(F16 x) { return static_cast<float>(__builtin_bit_cast(_Float16, x.bits)); }
+
+// One rounding, to nearest even, of the finished 32-bit value.
+__device__ __forceinline__ void narrow(float v, float& o) { o = v; }
+__device__ __forceinline__ void narrow(float v, Bf16& o) { o.bits = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); }
+__device__ __forceinline__ void narrow(float v, F16& o) { o.bits = __builtin_bit_cast(uint16_t, static_cast<_Float16>(v)); }
+
+template <class T>
+constexpr int kChunk = 16 / sizeof(T);           // elements of a 16-byte chunk
+
+// A lane's elements of a row: chunk c of the lane starts at element (c * 8 + lane) * kChunk.  Elements past E come as -inf.
+// vec: 16 or 8 where every row starts at a multiple of it and holds a whole number of such pieces, else the element's size.
+template <class T, int CH>
+__device__ __forceinline__ void load_row(const T* row, int sub, int E, int vec, float (&x)[CH * kChunk<T>]) {
+  constexpr int V = kChunk<T>;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int at = (c * kRowLanes + sub) * V;
+    alignas(16) T piece[V];
+    if (vec == 16) {
+      if (at < E) *reinterpret_cast<uint4*>(piece) = *reinterpret_cast<const uint4*>(row + at);
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[c * V + j] = at < E ? widen(piece[j]) : kNone;
+    } else if (vec == 8) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int a = at + h * (V / 2);
+        if (a < E) *reinterpret_cast<uint2*>(piece + h * (V / 2)) = *reinterpret_cast<const uint2*>(row + a);
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) x[c * V + h * (V / 2) + j] = a < E ? widen(piece[h * (V / 2) + j]) : kNone;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[c * V + j] = at + j < E ? widen(row[at + j]) : kNone;
+    }
+  }
+}
+
+template <class T, int CH>
+__device__ __forceinline__ void store_row(T* row, int sub, int E, int vec, const float (&x)[CH * kChunk<T>]) {
+  constexpr int V = kChunk<T>;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int at = (c * kRowLanes + sub) * V;
+    alignas(16) T piece[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) narrow(x[c * V + j], piece[j]);
+    if (vec == 16) {
+      if (at < E) *reinterpret_cast<uint4*>(row + at) = *reinterpret_cast<uint4*>(piece);
+    } else if (vec == 8) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (at + h * (V / 2) < E)
+          *reinterpret_cast<uint2*>(row + at + h * (V / 2)) = *reinterpret_cast<uint2*>(piece + h * (V / 2));
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (at + j < E) row[at + j] = piece[j];
+    }
+  }
+}
+
+__device__ __forceinline__ float row_max(float v) {
+#pragma unroll
+  for (int o = 1; o < kRowLanes; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ float row_sum(float v) {
+#pragma unroll
+  for (int o = 1; o < kRowLanes; o <<= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
+
+struct Run {
+  int family;
+  int64_t first, last;  // tokens
+};
+template <class Args>
+__device__ __forceinline__ Run run_of(const Args& a, int run) {
+  int f = 0;
+  while (run >= a.run_off[f + 1]) ++f;
+  Run r;
+  r.family = f;
+  r.first = a.fam_off[f] + static_cast<int64_t>(run - a.run_off[f]) * a.rows;
+  const int64_t end = r.first + a.rows;
+  r.last = end < a.fam_off[f + 1] ? end : a.fam_off[f + 1];
+  return r;
+}
+
+// grid: (runs, layers).  KS: slots that a lane of a row takes (ids sub and sub + 8).
+template <class T, int CH, int KS, bool BAL>
+__global__ __launch_bounds__(kRouteThreads) void route_main(RouteArgs a) {
+  constexpr int V = kChunk<T>, M = CH * V;
+  __shared__ uint32_t count[BAL ? TACG_MAX_EXPERTS : 1];
+  __shared__ float mass[BAL ? kRouteWaves : 1][BAL ? TACG_MAX_EXPERTS : 1];
+  __shared__ float squares[kRouteWaves];
+  __shared__ uint32_t routed[kRouteWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & (kRowLanes - 1);
+  const int l = blockIdx.y;
+  const Run run = run_of(a, blockIdx.x);
+  const int E = a.E, k = a.k;
+  const T* layer = static_cast<const T*>(a.logits) + l * a.stride_layer;
+  float acc[BAL ? M : 1];
+  float sq = 0.0f;
+  uint32_t live = 0;
+  if (BAL) {
+#pragma unroll
+    for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] = 0.0f;
+    for (int e = tid; e < E; e += kRouteThreads) count[e] = 0;
+    __syncthreads();
+  }
+  for (int64_t base = run.first; base < run.last; base += kRowsPerPass) {
+    const int64_t t = base + (tid >> 3);
+    const bool in = t < run.last;
+    const T* row = layer + (in ? t : run.first) * a.stride_token;
+    float x[M];
+    load_row<T, CH>(row, sub, E, a.vec, x);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < M; ++i) bad |= !(x[i] < INFINITY);
+    if (__any(bad)) {  // a NaN or +inf: the row is not routed
+      const uint64_t m = __ballot(bad) >> (lane & ~(kRowLanes - 1));
+      if ((m & 0xff) != 0) {
+        if (in && sub == 0) atomicOr(a.err, TACG_ERR_VALUE);
+#pragma unroll
+        for (int i = 0; i < M; ++i) x[i] = kNone;
+      }
+    }
+    // scores: p = exp(x - max) (softmax, to be divided by their sum) or the sigmoid
+    float top = kNone, total = 0.0f, p[M];
+    if (a.softmax) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) top = fmaxf(top, x[i]);
+      top = row_max(top);
+    }
+    const float shift = top == kNone ? 0.0f : top;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      p[i] = a.softmax ? __expf(x[i] - shift) : sigmoid(x[i]);
+      total += p[i];
+    }
+    total = row_sum(total);
+    const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
+    // selection: by the logit itself, which orders as its score, or by score + bias
+    float y[M];
+#pragma unroll
+    for (int i = 0; i < M; ++i) y[i] = x[i] + 0.0f;  // -0 and +0 are equal
+    if (a.bias != nullptr) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const int e = (c * kRowLanes + sub) * V + j, i = c * V + j;
+          const float s = a.softmax ? p[i] * inverse : p[i];
+          y[i] = x[i] > kNone ? s + a.bias[l * E + (e < E ? e : 0)] : kNone;
+        }
+    }
+    int id[KS];
+#pragma unroll
+    for (int q = 0; q < KS; ++q) id[q] = -1;
+    float last = INFINITY;
+    int last_e = -1;
+    for (int j = 0; j < k; ++j) {  // the best after the last winner in (value descending, id ascending)
+      float best = kNone;
+      int at = 0x7fffffff;
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          const int e = (c * kRowLanes + sub) * V + q;
+          const float v = y[c * V + q];
+          const bool after = v < last || (v == last && e > last_e);
+          if (after && v > best) best = v, at = e;
+        }
+#pragma unroll
+      for (int o = 1; o < kRowLanes; o <<= 1) {
+        const float v = __shfl_xor(best, o, 64);
+        const int e = __shfl_xor(at, o, 64);
+        if (v > best || (v == best && e < at)) best = v, at = e;
+      }
+      const int winner = best > kNone ? at : -1;
+#pragma unroll
+      for (int q = 0; q < KS; ++q)
+        if (j == sub + q * kRowLanes) id[q] = winner;
+      last = best > kNone ? best : kNone;
+      last_e = best > kNone ? at : 0x7fffffff;
+    }
+    // gates of the selected
+    float w[KS];
+#pragma unroll
+    for (int q = 0; q < KS; ++q) w[q] = id[q] >= 0 ? widen(row[id[q]]) : kNone;
+    if (a.softmax) {
+      float high = shift;
+      if (a.renorm) {
+        high = kNone;
+#pragma unroll
+        for (int q = 0; q < KS; ++q) high = fmaxf(high, w[q]);
+        high = row_max(high);
+        high = high == kNone ? 0.0f : high;
+      }
+#pragma unroll
+      for (int q = 0; q < KS; ++q) w[q] = __expf(w[q] - high);
+    } else {
+#pragma unroll
+      for (int q = 0; q < KS; ++q) w[q] = sigmoid(w[q]);
+    }
+    float factor = a.scale;
+    if (a.renorm) {
+      float part = 0.0f;
+#pragma unroll
+      for (int q = 0; q < KS; ++q) part += w[q];
+      part = row_sum(part);
+      factor = part > 0.0f ? a.scale / part : 0.0f;
+    } else if (a.softmax) {
+      factor = a.scale * inverse;
+    }
+    const int64_t at = static_cast<int64_t>(l) * a.n_tokens + t;
+#pragma unroll
+    for (int q = 0; q < KS; ++q) {
+      const int j = sub + q * kRowLanes;
+      if (in && j < k) {
+        a.trace[at * k + j] = static_cast<int16_t>(id[q]);
+        a.gate[at * k + j] = w[q] * factor;
+        if (BAL && id[q] >= 0) atomicAdd(&count[id[q]], 1u);
+      }
+    }
+    const bool some = __shfl(id[0], lane & ~(kRowLanes - 1), 64) >= 0;
+    const float norm = a.softmax ? (some ? top + __logf(total) : kNone) : total;
+    if (a.norm != nullptr && in && sub == 0) a.norm[at] = norm;
+    if (BAL && in && some) {
+#pragma unroll
+      for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] += p[i] * inverse;
+      if (sub == 0) {
+        live += 1;
+        if (a.softmax) sq += norm * norm;
+      }
+    }
+  }
+  if (!BAL) return;
+  // the run's sums: rows of a wave, then the waves in order
+#pragma unroll
+  for (int i = 0; i < (BAL ? M : 1); ++i) {
+#pragma unroll
+    for (int o = kRowLanes; o < 64; o <<= 1) acc[i] += __shfl_xor(acc[i], o, 64);
+    const int e = ((i / V) * kRowLanes + sub) * V + i % V;
+    if (lane < kRowLanes && e < E) mass[wave][e] = acc[i];
+  }
+#pragma unroll
+  for (int o = kRowLanes; o < 64; o <<= 1) {
+    sq += __shfl_xor(sq, o, 64);
+    live += __shfl_xor(live, o, 64);
+  }
+  if (lane == 0) squares[wave] = sq, routed[wave] = live;
+  barrier_after_lds_atomics();
+  const int64_t slot = static_cast<int64_t>(l) * gridDim.x + blockIdx.x;
+  for (int e = tid; e < E; e += kRouteThreads) {
+    float m = mass[0][e];
+#pragma unroll
+    for (int w = 1; w < (BAL ? kRouteWaves : 1); ++w) m += mass[w][e];
+    a.mass[slot * E + e] = m;
+    a.count[slot * E + e] = count[e];
+  }
+  if (tid == 0) {
+    double s = 0.0;
+    uint32_t n = 0;
+#pragma unroll
+    for (int w = 0; w < kRouteWaves; ++w) s += squares[w], n += routed[w];
+    a.squares[slot] = s;
+    a.routed[slot] = n;
+  }
+}
+
+struct ReduceArgs {
+  const float* mass;
+  const uint32_t* count;
+  const double* squares;
+  const uint32_t* routed;
+  int32_t runs, L, E, k;
+  uint32_t* D;
+  uint32_t* tokens;
+  float* balance;
+  float* z;
+  int32_t run_off[TACG_MAX_FAMILIES + 1];
+};
+
+// grid: (families, layers), a thread per expert.
+__global__ __launch_bounds__(TACG_MAX_EXPERTS) void route_reduce(ReduceArgs a) {
+  __shared__ double part[TACG_MAX_EXPERTS / 64];
+  const int f = blockIdx.x, l = blockIdx.y, e = threadIdx.x, lane = e & 63, wave = e >> 6;
+  const int64_t segment = static_cast<int64_t>(f) * a.L + l;
+  const int64_t from = static_cast<int64_t>(l) * a.runs;
+  double m = 0.0, s = 0.0;
+  uint32_t c = 0, n = 0;
+  for (int r = a.run_off[f]; r < a.run_off[f + 1]; ++r) {
+    const int64_t slot = from + r;
+    if (e < a.E) {
+      m += a.mass[slot * a.E + e];
+      c += a.count[slot * a.E + e];
+    }
+    s += a.squares[slot];
+    n += a.routed[slot];
+  }
+  if (e < a.E) a.D[segment * a.E + e] = c;
+  double v = m * c;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  if (lane == 0) part[wave] = v;
+  __syncthreads();
+  if (e == 0) {
+    double b = 0.0;
+    for (int w = 0; w < TACG_MAX_EXPERTS / 64; ++w) b += part[w];
+    const double rows = n;
+    a.tokens[segment] = n;
+    a.balance[segment] = n ? static_cast<float>(b * a.E / (a.k * rows * rows)) : 0.0f;
+    if (a.z != nullptr) a.z[segment] = n ? static_cast<float>(s / rows) : 0.0f;
+  }
+}
+
+template <class T, int CH, int KS>
+__global__ __launch_bounds__(kRouteThreads) void route_back(BackArgs a) {
+  constexpr int V = kChunk<T>, M = CH * V, kStride = M * kRowLanes + 32;
+  __shared__ float sparse[kRowsPerPass][kStride];  // gradient of the scores of a row's selected experts, else 0
+  const int tid = threadIdx.x, lane = tid & 63, sub = lane & (kRowLanes - 1);
+  const int l = blockIdx.y;
+  const Run run = run_of(a, blockIdx.x);
+  const int E = a.E, k = a.k;
+  const int64_t segment = static_cast<int64_t>(run.family) * a.n_layers + l;
+  const T* layer = static_cast<const T*>(a.logits) + l * a.stride_layer;
+  float* mine = sparse[tid >> 3];
+  for (int i = sub; i < kStride; i += kRowLanes) mine[i] = 0.0f;
+  float c[M], zc = 0.0f;
+  {
+    const float n = a.tokens != nullptr ? static_cast<float>(a.tokens[segment]) : 0.0f;
+    const float b = a.grad_balance != nullptr && n > 0.0f ? a.grad_balance[segment] * E / (k * n * n) : 0.0f;
+    if (a.grad_z != nullptr && n > 0.0f) zc = a.grad_z[segment] * 2.0f / n;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      const int e = ((i / V) * kRowLanes + sub) * V + i % V;
+      c[i] = b != 0.0f && e < E ? b * static_cast<float>(a.D[segment * E + e]) : 0.0f;
+    }
+  }
+  for (int64_t base = run.first; base < run.last; base += kRowsPerPass) {
+    const int64_t t = base + (tid >> 3);
+    const bool in = t < run.last;
+    const int64_t at = static_cast<int64_t>(l) * a.n_tokens + (in ? t : run.first);
+    const T* row = layer + (in ? t : run.first) * a.stride_token;
+    float p[M];
+    load_row<T, CH>(row, sub, E, a.vec, p);
+    const float norm = a.norm[at];
+    const bool live = a.softmax ? norm > kNone : norm > 0.0f;
+    int id[KS];
+    float u[KS], s[KS];
+#pragma unroll
+    for (int q = 0; q < KS; ++q) {
+      const int j = sub + q * kRowLanes;
+      id[q] = -1;
+      u[q] = s[q] = 0.0f;
+      if (a.grad_gate != nullptr && j < k) {
+        id[q] = a.trace[at * k + j];
+        if (static_cast<uint32_t>(id[q]) >= static_cast<uint32_t>(E)) id[q] = -1;
+        if (id[q] >= 0) {
+          u[q] = a.grad_gate[at * k + j];
+          s[q] = widen(row[id[q]]);
+        }
+      }
+    }
+    // softmax from differences to the row's largest: a normaliser of magnitude 1e4 would leave errors of 1e-3 in its exp
+    float top = kNone, inverse = 0.0f;
+    if (a.softmax) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) top = fmaxf(top, p[i]);
+      top = row_max(top);
+      float total = 0.0f;
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        p[i] = live ? __expf(p[i] - top) : 0.0f;
+        total += p[i];
+      }
+      total = row_sum(total);
+      inverse = live ? 1.0f / total : 0.0f;
+    }
+    // scores of the selected, and the gradient through the gates
+    if (a.softmax) {
+      float high = top;
+      if (a.renorm) {
+        high = kNone;
+#pragma unroll
+        for (int q = 0; q < KS; ++q) high = fmaxf(high, id[q] >= 0 ? s[q] : kNone);
+        high = row_max(high);
+      }
+#pragma unroll
+      for (int q = 0; q < KS; ++q) s[q] = id[q] >= 0 ? __expf(s[q] - high) * (a.renorm ? 1.0f : inverse) : 0.0f;
+    } else {
+#pragma unroll
+      for (int q = 0; q < KS; ++q) s[q] = id[q] >= 0 ? sigmoid(s[q]) : 0.0f;
+    }
+    float su = 0.0f;  // softmax without renormalisation: sum s u
+    if (a.renorm) {
+      float part = 0.0f, mean = 0.0f;
+#pragma unroll
+      for (int q = 0; q < KS; ++q) part += s[q], mean += s[q] * u[q];
+      part = row_sum(part);
+      const float inv = part > 0.0f ? 1.0f / part : 0.0f;
+      mean = row_sum(mean) * inv;
+      // softmax: straight to the logits, gate (g - mean); sigmoid: to the score
+#pragma unroll
+      for (int q = 0; q < KS; ++q) u[q] = a.scale * inv * (u[q] - mean) * (a.softmax ? s[q] : 1.0f);
+    } else {
+#pragma unroll
+      for (int q = 0; q < KS; ++q) u[q] *= a.scale, su += s[q] * u[q];
+      if (a.softmax) {
+        su = row_sum(su);
+#pragma unroll
+        for (int q = 0; q < KS; ++q) u[q] *= s[q];
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < KS; ++q)
+      if (id[q] >= 0) mine[id[q]] = u[q];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // all experts of the row
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      p[i] = a.softmax ? p[i] * inverse : sigmoid(p[i]);
+      dot += p[i] * c[i];
+    }
+    dot = row_sum(dot);
+    if (a.softmax) {
+      const float sub_all = (live ? zc * norm : 0.0f) - dot - (a.renorm ? 0.0f : su);
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        const int e = ((i / V) * kRowLanes + sub) * V + i % V;
+        p[i] = p[i] * (c[i] + sub_all) + mine[e];
+      }
+    } else {
+      const float inv = live ? 1.0f / norm : 0.0f;
+      dot *= inv;
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        const int e = ((i / V) * kRowLanes + sub) * V + i % V;
+        p[i] = p[i] * (1.0f - p[i]) * ((c[i] - dot) * inv + mine[e]);
+      }
+    }
+    if (in) store_row<T, CH>(static_cast<T*>(a.grad) + at * E, sub, E, a.vec, p);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int q = 0; q < KS; ++q)
+      if (id[q] >= 0) mine[id[q]] = 0.0f;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// Bytes that a load of a row's piece may take: rows start at a multiple of them and hold a whole number of pieces.
+int piece_bytes(const void* base, int64_t stride_layer, int64_t stride_token, int32_t E, int size) {
+  for (int b = 16; b >= 8; b /= 2) {
+    const int64_t n = b / size;
+    if (reinterpret_cast<uintptr_t>(base) % b == 0 && stride_layer % n == 0 && stride_token % n == 0 && E % n == 0)
+      return b;
+  }
+  return size;
+}
+
+int dtype_size(int32_t dtype) { return dtype == TACG_F32 ? 4 : 2; }
+
+// Rows of a workgroup's run: enough runs for the chip (eight workgroups a CU), of at least two passes where sums of a run go to a
+// slot (a slot is as long as two to four rows), and whole passes.
+int run_rows(int64_t total_rows, bool sums) {
+  int64_t r = total_rows / (256 * 8);
+  r = (r + kRowsPerPass - 1) / kRowsPerPass * kRowsPerPass;
+  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(r, sums ? 2 * kRowsPerPass : kRowsPerPass), 512));
+}
+
+template <class Args>
+int fill_runs(Args& a, const int64_t* fam_off_host, int32_t n_fam, int rows) {
+  int64_t runs = 0;
+  a.rows = rows;
+  for (int f = 0; f < n_fam; ++f) {
+    a.fam_off[f] = fam_off_host[f];
+    a.run_off[f] = static_cast<int32_t>(runs);
+    runs += (fam_off_host[f + 1] - fam_off_host[f] + rows - 1) / rows;
+  }
+  a.fam_off[n_fam] = fam_off_host[n_fam];
+  a.run_off[n_fam] = static_cast<int32_t>(runs);
+  return static_cast<int>(runs);
+}
+
+template <class T, int CH>
+void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
+  const bool two = a.k > kRowLanes;
+  auto* kernel = bal ? (two ? route_main<T, CH, 2, true> : route_main<T, CH, 1, true>)
+                     : (two ? route_main<T, CH, 2, false> : route_main<T, CH, 1, false>);
+  kernel<<<grid, kRouteThreads, 0, s>>>(a);
+}
+
+template <class T>
+void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
+  const int chunks = (a.E + kChunk<T> * kRowLanes - 1) / (kChunk<T> * kRowLanes);
+  if (chunks <= 1) start_main<T, 1>(a, bal, grid, s);
+  else if (chunks <= 2) start_main<T, 2>(a, bal, grid, s);
+  else if (chunks <= 4) start_main<T, 4>(a, bal, grid, s);
+  else if constexpr (sizeof(T) == 4) start_main<T, 8>(a, bal, grid, s);
+}
+
+template <class T, int CH>
+void start_back(const BackArgs& a, dim3 grid, hipStream_t s) {
+  auto* kernel = a.k > kRowLanes ? route_back<T, CH, 2> : route_back<T, CH, 1>;
+  kernel<<<grid, kRouteThreads, 0, s>>>(a);
+}
+
+template <class T>
+void start_back(const BackArgs& a, dim3 grid, hipStream_t s) {
+  const int chunks = (a.E + kChunk<T> * kRowLanes - 1) / (kChunk<T> * kRowLanes);
+  if (chunks <= 1) start_back<T, 1>(a, grid, s);
+  else if (chunks <= 2) start_back<T, 2>(a, grid, s);
+  else if (chunks <= 4) start_back<T, 4>(a, grid, s);
+  else if constexpr (sizeof(T) == 4) start_back<T, 8>(a, grid, s);
+}
+
+}  // namespace
+
+size_t route_workspace(int64_t n_tokens, int32_t n_layers, int32_t n_experts, int32_t n_fam) {
+  const int rows = run_rows(n_tokens * n_layers, true);
+  const size_t slots = static_cast<size_t>(n_layers) * static_cast<size_t>(n_tokens / rows + n_fam);
+  return 2 * align256(slots * n_experts * 4) + align256(slots * 8) + align256(slots * 4);
+}
+
+int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+                 int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+                 int32_t score, const float* bias, bool renorm, float scale, int16_t* trace, float* gate, float* norm,
+                 uint32_t* D, uint32_t* tokens, float* balance, float* z, uint32_t* d_err, void* workspace,
+                 hipStream_t stream) {
+  const bool bal = D != nullptr;
+  RouteArgs a{};
+  a.logits = logits;
+  a.stride_layer = stride_layer;
+  a.stride_token = stride_token;
+  a.n_tokens = n_tokens;
+  a.n_layers = n_layers;
+  a.E = n_experts;
+  a.k = top_k;
+  a.F = n_fam;
+  a.softmax = score == TACG_SOFTMAX;
+  a.renorm = renorm;
+  a.scale = scale;
+  a.bias = bias;
+  a.trace = trace;
+  a.gate = gate;
+  a.norm = norm;
+  a.err = d_err;
+  a.vec = piece_bytes(logits, stride_layer, stride_token, n_experts, dtype_size(dtype));
+  const int runs = fill_runs(a, fam_off_host, n_fam, run_rows(n_tokens * n_layers, bal));
+  if (bal) {
+    Carver w{static_cast<char*>(workspace), 0};
+    const size_t slots = static_cast<size_t>(n_layers) * runs;
+    a.mass = w.take<float>(slots * n_experts);
+    a.count = w.take<uint32_t>(slots * n_experts);
+    a.squares = w.take<double>(slots);
+    a.routed = w.take<uint32_t>(slots);
+  }
+  if (runs > 0) {
+    const dim3 grid(runs, n_layers);
+    if (dtype == TACG_F32) start_main<float>(a, bal, grid, stream);
+    else if (dtype == TACG_BF16) start_main<Bf16>(a, bal, grid, stream);
+    else start_main<F16>(a, bal, grid, stream);
+    if (hipGetLastError() != hipSuccess) return TACG_E_DEVICE;
+  }
+  if (bal) {
+    ReduceArgs r{};
+    r.mass = a.mass;
+    r.count = a.count;
+    r.squares = a.squares;
+    r.routed = a.routed;
+    r.runs = runs;
+    r.L = n_layers;
+    r.E = n_experts;
+    r.k = top_k;
+    r.D = D;
+    r.tokens = tokens;
+    r.balance = balance;
+    r.z = z;
+    for (int f = 0; f <= n_fam; ++f) r.run_off[f] = a.run_off[f];
+    route_reduce<<<dim3(n_fam, n_layers), TACG_MAX_EXPERTS, 0, stream>>>(r);
+    if (hipGetLastError() != hipSuccess) return TACG_E_DEVICE;
+  }
+  return TACG_OK;
+}
+
+int launch_route_backward(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token,
+                          int64_t n_tokens, int32_t n_layers, int32_t top_k, int32_t n_experts,
+                          const int64_t* fam_off_host, int32_t n_fam, int32_t score, bool renorm, float scale,
+                          const int16_t* trace, const float* norm, const uint32_t* D, const uint32_t* tokens,
+                          const float* grad_gate, const float* grad_balance, const float* grad_z, void* grad_logits,
+                          hipStream_t stream) {
+  BackArgs a{};
+  a.logits = logits;
+  a.stride_layer = stride_layer;
+  a.stride_token = stride_token;
+  a.n_tokens = n_tokens;
+  a.n_layers = n_layers;
+  a.E = n_experts;
+  a.k = top_k;
+  a.F = n_fam;
+  a.softmax = score == TACG_SOFTMAX;
+  a.renorm = renorm;
+  a.scale = scale;
+  a.trace = trace;
+  a.norm = norm;
+  a.D = D;
+  a.tokens = tokens;
+  a.grad_gate = grad_gate;
+  a.grad_balance = grad_balance;
+  a.grad_z = grad_z;
+  a.grad = grad_logits;
+  const int size = dtype_size(dtype);
+  a.vec = std::min(piece_bytes(logits, stride_layer, stride_token, n_experts, size),
+                   piece_bytes(grad_logits, 0, 0, n_experts, size));
+  const int runs = fill_runs(a, fam_off_host, n_fam, run_rows(n_tokens * n_layers, false));
+  if (runs == 0) return TACG_OK;
+  const dim3 grid(runs, n_layers);
+  if (dtype == TACG_F32) start_back<float>(a, grid, stream);
+  else if (dtype == TACG_BF16) start_back<Bf16>(a, grid, stream);
+  else start_back<F16>(a, grid, stream);
+  return hipGetLastError() == hipSuccess ? TACG_OK : TACG_E_DEVICE;
+}
+
+}  // namespace tacg

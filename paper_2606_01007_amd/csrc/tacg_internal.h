@@ -105,4 +105,29 @@ int launch_placement_load(const uint32_t* D, int32_t n_fam, int32_t n_layers, in
 int launch_jain(const uint32_t* load, int32_t n_place, int32_t n_layers, int32_t n_gpus, int32_t per_layer,
                 float* jain, float* maxvio, hipStream_t stream);
 
+// ---- router ----------------------------------------------------------------------------------
+size_t route_workspace(int64_t n_tokens, int32_t n_layers, int32_t n_experts, int32_t n_fam);
+int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+                 int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+                 int32_t score, const float* bias, bool renorm, float scale, int16_t* trace, float* gate, float* norm,
+                 uint32_t* D, uint32_t* tokens, float* balance, float* z, uint32_t* d_err, void* workspace,
+                 hipStream_t stream);
+int launch_route_backward(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token,
+                          int64_t n_tokens, int32_t n_layers, int32_t top_k, int32_t n_experts,
+                          const int64_t* fam_off_host, int32_t n_fam, int32_t score, bool renorm, float scale,
+                          const int16_t* trace, const float* norm, const uint32_t* D, const uint32_t* tokens,
+                          const float* grad_gate, const float* grad_balance, const float* grad_z, void* grad_logits,
+                          hipStream_t stream);
+
+// ---- experts' products with 4-bit weights ----------------------------------------------------
+int launch_q4_pack(const void* w, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t stride, int32_t group,
+                   int32_t scale_dtype, uint8_t* q, void* scales, uint8_t* zeros, uint32_t* d_err, hipStream_t stream);
+size_t expert_q4_workspace(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_rows, int32_t n_cols,
+                           int32_t mode);
+int launch_expert_q4(const void* x, int32_t dtype, int64_t x_stride_token, int64_t x_stride_slot, int64_t n_tokens,
+                     int32_t top_k, int32_t n_experts, const int16_t* ids, const int32_t* slot_of_expert,
+                     int32_t n_held, const uint8_t* q, const void* scales, const uint8_t* zeros, int32_t group,
+                     int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate, void* out, uint32_t* d_err,
+                     void* workspace, hipStream_t stream);
+
 }  // namespace tacg

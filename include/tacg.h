@@ -372,12 +372,12 @@ int tacg_q4_pack(const void* w, int32_t dtype, int64_t n_rows, int32_t n_cols, i
  * x(t, j) = the n_cols values from element t * stride_token + j * stride_slot of x (strides >= 0; 0 for one x per token).
  *   TACG_Q4_EACH  out[t][j][n] = W_h[n] . x(t, j)                                                    (out [T][k][n_rows])
  *   TACG_Q4_GLU   out[t][j][n] = silu(W_h[n] . x) * (W_h[n + n_rows / 2] . x)                        (out [T][k][n_rows / 2])
- *   TACG_Q4_SUM   out[t][n]    = sum over served j, in slot order, of gate[t][j] * (W_h[n] . x(t, j))  (out [T][n_rows])
+ *   TACG_Q4_SUM   out[t][n]    = sum over served j of gate[t][j] * (W_h[n] . x(t, j))            (out [T][n_rows])
  * with 0 for what is served elsewhere.  x, scales and out have type `dtype` (TACG_BF16 or TACG_F16), gate is float [T][k] (required for
  * TACG_Q4_SUM).  Products are exact in the levels, sums are held in 32 bits, and the result is rounded once; it does not depend on
  * the order of execution.  Data errors: TACG_ERR_ID_RANGE (id >= E or < -1), TACG_ERR_TABLE (h >= n_held); such slots are
  * taken as served elsewhere.  workspace: tacg_expert_q4_workspace_bytes(...) bytes (NULL where that is 0).
- * n_rows, n_cols <= TACG_MAX_WIDTH; T * k < 2^31.
+ * n_rows, n_cols <= TACG_MAX_WIDTH; T * k < 2^28.
  */
 int tacg_expert_q4(const void* x, int32_t dtype, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
                    int32_t top_k, int32_t n_experts, const int16_t* ids, const int32_t* slot_of_expert_or_null,

@@ -5,19 +5,18 @@
 // q4_pack_kernel: levels, scales and zeros of a weight matrix, a lane per 32 columns (16 bytes of levels).
 //
 // The products run on the matrix cores, with tokens as rows and weight rows as columns of v_mfma_f32_16x16x32: lane n + 16 q supplies
-// columns 8 q .. 8 q + 7 of weight row n and of token n, and holds the sums of weight row n with tokens 4 q .. 4 q + 3.  A step is 128
-// columns of 16 weight rows: a lane loads 16 bytes, columns 32 q .. 32 q + 31 of its row, and two exchanges of half and quarter waves
-// give it the words of the four products of the step, each of 32 columns.  (Without the exchange the tokens' loads would be spread over
-// four times as many cache lines.)  A level becomes a 16-bit float by an OR into the mantissa: 128 + level (bfloat16) or
-// 1024 + level (float16), both exact; the float16 one is then brought to level - zero by one exact packed subtraction, the bfloat16
-// one after the product: sum (level - zero) x = sum (128 + level) x - (128 + zero) sum x, with sum x from a product with ones.
-// The eight levels of a word come out in the order 0 4 1 5 2 6 3 7, so the tokens' values are put in that order too.  The scale of a
-// group is applied in 32 bits to the group's sum.
+// columns 8 q .. 8 q + 7 of weight row n and of token n, and holds the sums of weight row n with tokens 4 q .. 4 q + 3.  A step is 256
+// columns of 16 weight rows: a lane loads twice 16 bytes, columns 32 q .. 32 q + 31 of 128, and exchanges of half and quarter waves
+// give it the words of the step's products, each of 32 columns.  (Without the exchange the tokens' loads would be spread over
+// four times as many cache lines.)  A level becomes a 16-bit float by an AND-OR into the mantissa, as offset + level, which is exact; the
+// offset and the zero are taken off the group's sum:  sum (level - zero) x = sum (offset + level) x - (offset + zero) sum x,  with sum x
+// from a product with ones.  The eight levels of a word come out in the order 0 4 1 5 2 6 3 7, so the tokens' values are put in
+// that order too.  The scale of a group is applied in 32 bits to the group's sum.
 //
-// The waves of a workgroup take the steps of its 16 RT weight rows in turn and add their sums up in LDS, in order.
-// q4_tiles: a workgroup finds the tokens of its expert by itself (no launch before it): with few (token, slot) pairs it is the one of
-//   the first pair of that expert, with many there is a workgroup for each held expert.
-// q4_sum_token: few pairs, summed over a token's experts: a workgroup takes all experts of one token, the steps of all of them in turn.
+// q4_tiles: many (token, slot) pairs.  A workgroup takes an expert and a block of its weight rows and finds the expert's tokens by itself
+//   (no launch before it); every wave has rows of its own.
+// q4_few: few pairs.  A workgroup takes 16 weight rows (gated: 16 pairs of them) of the expert of one pair, or, summed, of all experts of a
+//   token; its waves take the steps in turn and add their sums up in LDS, in order.
 // q4_combine: sums the 32-bit products of many pairs over the slots of a token.
 #include <algorithm>
 #include <cmath>
@@ -40,7 +39,6 @@ struct Q4Args {
   const void* scales;
   const uint8_t* zeros;     // or null
   const float* gate;        // [T][k] or null
-  int32_t few;              // few pairs: a workgroup per pair and block of rows
   float* part;              // [T][k][N], or null
   void* out;
   uint32_t* err;
@@ -61,9 +59,8 @@ __device__ __forceinline__ void report(const Q4Args& a, int h) {
   if (h == kBadTable) atomicOr(a.err, TACG_ERR_TABLE);
 }
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * 64;
-constexpr int kStep = 128;       // columns of a step
+constexpr int kStep = 256;       // columns of a step
+constexpr int kBlocks = kStep / 32;
 constexpr int kScan = 8192;      // pairs that a workgroup looks through
 
 typedef __attribute__((ext_vector_type(4))) float float4v;
@@ -81,155 +78,200 @@ __device__ __forceinline__ float4v mfma(const uint4v& tokens, const uint4v& weig
                                                 c, 0, 0, 0);
 }
 
-// 16-bit floats of the eight levels of a word, in the order 0 4 1 5 2 6 3 7: 128 + level.
-__device__ __forceinline__ uint4v spread(uint32_t w, uint32_t, __bf16) {
-  constexpr uint32_t kMask = 0x000f000fu, kBase = 0x43004300u;
-  return uint4v{(w & kMask) | kBase, ((w >> 4) & kMask) | kBase, ((w >> 8) & kMask) | kBase, ((w >> 12) & kMask) | kBase};
+// 16-bit floats offset + level of the eight levels of a word, in the order 0 4 1 5 2 6 3 7: four bits under the mantissa's bit of
+// weight 1.  A level in bits 4 to 7 needs an offset of 64 in float16, in bits 0 to 3 one of 1024, which would cost the sums four bits.
+template <class T>
+constexpr float kOffset = __is_same(T, __bf16) ? 128.0f : 64.0f;
+template <class T>
+__device__ __forceinline__ uint4v spread(uint32_t w) {
+  uint32_t mask;  // in a vector register: an AND-OR takes one scalar operand
+  if constexpr (__is_same(T, __bf16)) {
+    asm("v_mov_b32 %0, 0xf000f" : "=v"(mask));
+    constexpr uint32_t kBase = 0x43004300u;
+    return uint4v{(w & mask) | kBase, ((w >> 4) & mask) | kBase, ((w >> 8) & mask) | kBase, ((w >> 12) & mask) | kBase};
+  } else {
+    asm("v_mov_b32 %0, 0xf000f0" : "=v"(mask));
+    constexpr uint32_t kBase = 0x54005400u;
+    return uint4v{((w << 4) & mask) | kBase, (w & mask) | kBase, ((w >> 4) & mask) | kBase, ((w >> 8) & mask) | kBase};
+  }
 }
-// The same as level - zero; `minus` holds -(1024 + zero) twice.
-__device__ __forceinline__ uint4v spread(uint32_t w, uint32_t minus, _Float16) {
-  constexpr uint32_t kMask = 0x000f000fu, kBase = 0x64006400u;
-  const f16x2 m = __builtin_bit_cast(f16x2, minus);
-  uint4v o;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    o[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, ((w >> (4 * i)) & kMask) | kBase) + m);
+
+// The matrix that a workgroup reads, and where a lane's rows lie in it.
+template <class T, int RT>
+struct Rows {
+  const char* level;
+  const T* scale;
+  const uint8_t* zero;
+  uint32_t at[RT];  // row
+};
+
+// A step's weights of a lane, as loaded.  GROUPS: scale groups of a step, two scales and four zeros to a word.
+template <class T, int RT, int GROUPS>
+struct Weights {
+  uint4v level[RT][2];
+  uint32_t scale[RT][(GROUPS + 1) / 2];
+  uint32_t zero[RT][(GROUPS + 3) / 4];
+};
+
+template <class T, int RT>
+__device__ __forceinline__ Rows<T, RT> rows_of(const Q4Args& a, int h) {
+  const int64_t first = static_cast<int64_t>(h < 0 ? 0 : h) * a.N;
+  Rows<T, RT> o;
+  o.level = reinterpret_cast<const char*>(a.q) + first * a.pieces * 16;
+  o.scale = static_cast<const T*>(a.scales) + first * a.n_groups;
+  o.zero = a.zeros + first * a.n_groups;
   return o;
 }
 
-// One step's operands of a lane, as loaded.  PER: groups of a step.
-template <class T, int RT, int TT, int PER>
-struct Operands {
-  uint4v w[RT];
-  T scale[RT][PER];
-  uint8_t zero[RT][PER];
-  uint4v x[TT][4];
-};
-
-// row: first byte-piece index of each weight row; x: the lane's token rows, null where there is none.
-template <class T, int RT, int TT, int PER>
-__device__ __forceinline__ void load_step(const Q4Args& a, int s, int quarter, const int64_t (&row)[RT],
-                                          const T* const (&x)[TT], Operands<T, RT, TT, PER>& o) {
-  int piece = 4 * s + quarter;  // past the end the tokens' values are 0: any levels do
-  piece = piece < a.pieces ? piece : a.pieces - 1;
-#pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    o.w[i] = reinterpret_cast<const uint4v*>(a.q)[row[i] * a.pieces + piece];
-#pragma unroll
-    for (int g = 0; g < PER; ++g) {
-      int at = PER == 1 ? s * kStep / a.group : s * PER + g;
-      at = at < a.n_groups ? at : a.n_groups - 1;
-      o.scale[i][g] = static_cast<const T*>(a.scales)[row[i] * a.n_groups + at];
-      o.zero[i][g] = a.zeros != nullptr ? a.zeros[row[i] * a.n_groups + at] : 8;
+// The words of N values of a row's groups from `first` on; past the row's end any that can be read safely (the tokens' values are 0 there).
+template <int N, class V, int W>
+__device__ __forceinline__ void load_groups(const V* row, int first, int n_groups, uint32_t (&o)[W]) {
+  constexpr int kBits = 8 * sizeof(V);
+  if (n_groups >= N) {
+    const int from = first + N <= n_groups ? first : n_groups - N, skip = (first - from) * kBits;
+    if constexpr (N * sizeof(V) < 4) {
+      o[0] = 0;
+      __builtin_memcpy(o, row + from, N * sizeof(V));
+    } else {
+      __builtin_memcpy(o, row + from, sizeof(o));
     }
-  }
+    if (skip > 0) {  // the last step: bring the first group to the front
 #pragma unroll
-  for (int t = 0; t < TT; ++t)
+      for (int w = 0; w < W; ++w) {
+        uint32_t v = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = s * kStep + 32 * i + 8 * quarter;
-      o.x[t][i] = uint4v{0, 0, 0, 0};
-      if (x[t] != nullptr) {
-        if (c + 8 <= a.K) {
-          __builtin_memcpy(&o.x[t][i], x[t] + c, 16);  // rows need not be aligned to more than an element
-        } else if (c < a.K) {
-          T v[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = c + j < a.K ? x[t][c + j] : static_cast<T>(0.0f);
-          __builtin_memcpy(&o.x[t][i], v, 16);
+        for (int u = 0; u + w < W; ++u) {
+          const int by = skip - 32 * u;
+          if (by >= 0 && by < 32) v = o[w + u] >> by;
+          if (by < 0 && by > -32) v |= o[w + u] << -by;
         }
+        o[w] = v;
       }
     }
+  } else {
+#pragma unroll
+    for (int w = 0; w < W; ++w) o[w] = 0;
+#pragma unroll
+    for (int g = 0; g < N; ++g) {
+      V v = row[first + g < n_groups ? first + g : n_groups - 1];
+      uint32_t bits = 0;
+      __builtin_memcpy(&bits, &v, sizeof(V));
+      o[g * kBits / 32] |= bits << (g * kBits % 32);
+    }
+  }
 }
 
-// sum += factor * scale * (level - zero) . x of one step.
-template <class T, int RT, int TT, int PER>
-__device__ __forceinline__ void add_step(const Operands<T, RT, TT, PER>& o, float factor, float4v (&sum)[RT][TT]) {
-  constexpr bool kLate = sizeof(T) == 2 && __is_same(T, __bf16);  // the zero is taken off the sums
-  constexpr int kRun = 4 / PER;                                   // products of a group
-  uint4v x[TT][4];
+template <class T, int RT, int GROUPS>
+__device__ __forceinline__ void load_weights(const Q4Args& a, int s, int quarter, const Rows<T, RT>& rows,
+                                             Weights<T, RT, GROUPS>& o) {
 #pragma unroll
-  for (int t = 0; t < TT; ++t)
+  for (int i = 0; i < 2; ++i) {
+    int piece = 8 * s + 4 * i + quarter;  // past the end the tokens' values are 0: any levels do
+    piece = piece < a.pieces ? piece : a.pieces - 1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4v v = o.x[t][i];
-      x[t][i] = uint4v{__builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[2], v[0], 0x07060302u),
-                       __builtin_amdgcn_perm(v[3], v[1], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u)};
-    }
-  uint32_t w[RT][4];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const auto a = __builtin_amdgcn_permlane32_swap(o.w[r][0], o.w[r][2], false, false);
-    const auto b = __builtin_amdgcn_permlane32_swap(o.w[r][1], o.w[r][3], false, false);
-    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
-    const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    w[r][0] = c[0];
-    w[r][1] = c[1];
-    w[r][2] = d[0];
-    w[r][3] = d[1];
+    for (int r = 0; r < RT; ++r)
+      o.level[r][i] = *reinterpret_cast<const uint4v*>(rows.level + 16u * (rows.at[r] * a.pieces + piece));
   }
 #pragma unroll
-  for (int g = 0; g < PER; ++g) {
+  for (int r = 0; r < RT; ++r) {
+    load_groups<GROUPS>(rows.scale + rows.at[r] * a.n_groups, s * GROUPS, a.n_groups, o.scale[r]);
+    if (a.zeros != nullptr) {
+      load_groups<GROUPS>(rows.zero + rows.at[r] * a.n_groups, s * GROUPS, a.n_groups, o.zero[r]);
+    } else {
+#pragma unroll
+      for (int w = 0; w < (GROUPS + 3) / 4; ++w) o.zero[r][w] = 0x08080808u;
+    }
+  }
+}
+
+// Eight values of a token from column c on, 0 past the columns' end; `whole`: the step has no end in it.
+template <class T>
+__device__ __forceinline__ uint4v load_token(const Q4Args& a, const T* x, int c, bool whole) {
+  uint4v o = {0, 0, 0, 0};
+  if (whole || c + 8 <= a.K) {
+    __builtin_memcpy(&o, x + c, 16);  // rows need not be aligned to more than an element
+  } else if (c < a.K) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint16_t v = 0;
+      if (c + j < a.K) __builtin_memcpy(&v, x + c + j, 2);
+      o[j / 2] |= static_cast<uint32_t>(v) << (16 * (j % 2));
+    }
+  }
+  return o;
+}
+
+// The order in which spread() gives the levels.
+__device__ __forceinline__ uint4v in_order(const uint4v& v) {
+  return uint4v{__builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[2], v[0], 0x07060302u),
+                __builtin_amdgcn_perm(v[3], v[1], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u)};
+}
+
+template <class T>
+__device__ __forceinline__ float half_of(uint32_t word, int i) {
+  return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(word >> (16 * i))));
+}
+
+// sum += factor * scale * (level - zero) . x of one step; tokens(t, i): the lane's ordered values of block i of token tile t.
+template <class T, int RT, int TT, int GROUPS, class Tokens>
+__device__ __forceinline__ void add_step(const Weights<T, RT, GROUPS>& o, Tokens tokens, float factor,
+                                         float4v (&sum)[RT][TT]) {
+  constexpr int kRun = kBlocks / GROUPS;  // products of a group
+  constexpr uint32_t kOnes = __is_same(T, __bf16) ? 0x3f803f80u : 0x3c003c00u;
+  uint32_t w[RT][kBlocks];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4v l = o.level[r][i];
+      const auto a = __builtin_amdgcn_permlane32_swap(l[0], l[2], false, false);
+      const auto b = __builtin_amdgcn_permlane32_swap(l[1], l[3], false, false);
+      const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+      const auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+      w[r][4 * i] = c[0];
+      w[r][4 * i + 1] = c[1];
+      w[r][4 * i + 2] = d[0];
+      w[r][4 * i + 3] = d[1];
+    }
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g) {
     float4v all[TT], part[RT][TT];
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       all[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-      if (kLate) {
-        constexpr uint32_t kOnes = 0x3f803f80u;
 #pragma unroll
-        for (int i = g * kRun; i < (g + 1) * kRun; ++i) all[t] = mfma(x[t][i], uint4v{kOnes, kOnes, kOnes, kOnes}, all[t], T());
+      for (int r = 0; r < RT; ++r) part[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int i = g * kRun; i < (g + 1) * kRun; ++i) {
+      uint4v x[TT];
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        x[t] = tokens(t, i);
+        all[t] = mfma(x[t], uint4v{kOnes, kOnes, kOnes, kOnes}, all[t], T());
+      }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        const uint4v v = spread<T>(w[r][i]);
+#pragma unroll
+        for (int t = 0; t < TT; ++t) part[r][t] = mfma(x[t], v, part[r][t], T());
       }
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const uint32_t minus = 0xe400u + o.zero[r][g];  // -(1024 + zero) in float16
+      const float scale = half_of<T>(o.scale[r][g / 2], g % 2) * factor;
+      const float zero = kOffset<T> + static_cast<float>((o.zero[r][g / 4] >> (8 * (g % 4))) & 255u);
 #pragma unroll
-      for (int t = 0; t < TT; ++t) part[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int t = 0; t < TT; ++t) {
 #pragma unroll
-      for (int i = g * kRun; i < (g + 1) * kRun; ++i) {
-        const uint4v v = spread(w[r][i], minus | minus << 16, T());
-#pragma unroll
-        for (int t = 0; t < TT; ++t) part[r][t] = mfma(x[t][i], v, part[r][t], T());
+        for (int j = 0; j < 4; ++j) sum[r][t][j] += scale * (part[r][t][j] - zero * all[t][j]);
+        asm volatile("" : "+v"(sum[r][t]));  // here, and not with the other groups: all their products would not fit the registers
       }
-      const float scale = static_cast<float>(o.scale[r][g]) * factor;
-      const float zero = 128.0f + static_cast<float>(o.zero[r][g]);
-#pragma unroll
-      for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float v = kLate ? part[r][t][j] - zero * all[t][j] : part[r][t][j];
-          sum[r][t][j] += scale * v;
-        }
     }
   }
 }
 
 __device__ __forceinline__ float silu(float v) { return v / (1.0f + __expf(-v)); }
-
-// Adds the waves' sums of 16 tokens up in order; out(token, column) takes the value of each.
-template <int RT, int WIDTH, class Out>
-__device__ __forceinline__ void join(float (&red)[kWaves][16][RT * 16 + 4], const float4v (&mine)[RT], bool glu, Out out) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  __syncthreads();
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) red[wave][4 * (lane >> 4) + j][16 * r + (lane & 15)] = mine[r][j];
-  __syncthreads();
-  for (int i = tid; i < 16 * WIDTH; i += kThreads) {
-    const int t = i / WIDTH, n = i % WIDTH;
-    float v = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) v += red[w][t][n];
-    if (glu) {
-      float u = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) u += red[w][t][n + WIDTH];
-      v = silu(v) * u;
-    }
-    out(t, n, v);
-  }
-}
 
 __device__ __forceinline__ int look_up(const Q4Args& a, const int16_t* place, int id) {
   return static_cast<uint32_t>(id) < static_cast<uint32_t>(a.E) ? place[id] : id == -1 ? -1 : kBadId;
@@ -240,14 +282,27 @@ __device__ __forceinline__ int served_by(const Q4Args& a, const int16_t* place, 
 }
 
 // Where the pairs from `from` on, `n` of them, that matrix `h` serves (h = -1: that no matrix serves) stand in the list, in order.
+// A thread takes 8 V neighbouring ids, all loaded before the first is looked at.
+template <int V, int WAVES>
 __device__ __forceinline__ int list_pairs(const Q4Args& a, int64_t from, int n, int h, const int16_t* place,
-                                          uint16_t* list, int (&total)[kWaves]) {
+                                          uint16_t* list, int (&total)[WAVES]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int each = (n + kThreads - 1) / kThreads;
-  const int first = tid * each, last = first + each < n ? first + each : n;
-  int mine = 0;
-  for (int i = first; i < last; ++i) mine += served_by(a, place, a.ids[from + i]) == h;
-  int at = mine;
+  const int first = tid * 8 * V;
+  int16_t ids[8 * V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int16_t* p = a.ids + from + first + 8 * v;
+    if (first + 8 * v + 8 <= n) {
+      __builtin_memcpy(ids + 8 * v, p, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ids[8 * v + i] = first + 8 * v + i < n ? p[i] : -1;
+    }
+  }
+  uint32_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < 8 * V; ++i) mine |= (first + i < n && served_by(a, place, ids[i]) == h ? 1u : 0u) << i;
+  int at = __popc(mine);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int v = __shfl_up(at, o, 64);
@@ -255,50 +310,59 @@ __device__ __forceinline__ int list_pairs(const Q4Args& a, int64_t from, int n, 
   }
   if (lane == 63) total[wave] = at;
   __syncthreads();
-  at -= mine;
+  at -= __popc(mine);
   int all = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     if (w < wave) at += total[w];
     all += total[w];
   }
-  if (mine > 0)
-    for (int i = first; i < last; ++i)
-      if (served_by(a, place, a.ids[from + i]) == h) list[at++] = static_cast<uint16_t>(i);
+  while (mine != 0) {
+    list[at++] = static_cast<uint16_t>(first + __ffs(mine) - 1);
+    mine &= mine - 1;
+  }
   __syncthreads();
   return all;
 }
 
-// grid: (blocks of 16 RT weight rows; GLU: of half as many output columns, few pairs: pairs, many: held experts and one for the pairs
-// that none serves, runs of kScan pairs).
-template <class T, bool GLU, int RT, int TT, int PER>
-__global__ __launch_bounds__(kThreads) void q4_tiles(Q4Args a) {
-  constexpr int kWidth = GLU ? RT * 8 : RT * 16;  // output columns of a workgroup
-  __shared__ float red[kWaves][16][RT * 16 + 4];
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * 64;
+constexpr int kTokenBytes = kStep * 2 + 16;  // of a token's step in LDS: 16 tokens' pieces lie in different banks
+
+// Many pairs.  grid: (blocks of a workgroup's output columns, held experts and one for the pairs that none serves, runs of kScan pairs).
+// Every wave has weight rows of its own; the tokens' values come through LDS, a step ahead, in two buffers.
+template <class T, bool GLU, int RT, int TT, int GROUPS>
+__global__ __launch_bounds__(kThreads, 2) void q4_tiles(Q4Args a) {
+  constexpr int kOut = GLU ? RT * 8 : RT * 16;  // output columns of a wave
+  constexpr int kWidth = kOut * kWaves;         // of the workgroup
+  constexpr int kLoads = 2 * TT;                // 16-byte pieces of a step's tokens that a thread brings
+  __shared__ alignas(16) char held[2][16 * TT][kTokenBytes];
   __shared__ uint16_t list[kScan];
   __shared__ int16_t place[TACG_MAX_EXPERTS];
   __shared__ int total[kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, quarter = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t pairs = a.n_tokens * a.k, from = static_cast<int64_t>(blockIdx.z) * kScan;
   const int n = static_cast<int>(pairs - from < kScan ? pairs - from : kScan);
   for (int e = tid; e < a.E; e += kThreads) place[e] = static_cast<int16_t>(place_of(a, e));
-  __syncthreads();
-  int h;
-  if (a.few) {
-    h = look_up(a, place, a.ids[blockIdx.y]);
-    if (blockIdx.x == 0 && tid == 0) report(a, h);
-    h = h < 0 ? -1 : h;
-  } else {
-    h = static_cast<int>(blockIdx.y) < a.H ? static_cast<int>(blockIdx.y) : -1;
-    if (h < 0 && blockIdx.x == 0)
-      for (int i = tid; i < n; i += kThreads) report(a, look_up(a, place, a.ids[from + i]));
-  }
-  const int count = list_pairs(a, from, n, h, place, list, total);
-  if (count == 0 || (a.few && list[0] != blockIdx.y)) return;
+  const int h = static_cast<int>(blockIdx.y) < a.H ? static_cast<int>(blockIdx.y) : -1;
   const int column = blockIdx.x * kWidth;
   const int width = GLU ? a.N / 2 : a.N;
+  const int steps = (a.K + kStep - 1) / kStep;
+  Rows<T, RT> rows = rows_of<T, RT>(a, h);
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    int v = column + wave * kOut + 16 * (GLU ? r % (RT / 2) : r) + (lane & 15);
+    v = v < width ? v : width - 1;
+    rows.at[r] = v + (GLU && r >= RT / 2 ? width : 0);
+  }
+  __syncthreads();
+  const int count = n <= kThreads * 8 ? list_pairs<1>(a, from, n, h, place, list, total)
+                                      : list_pairs<4>(a, from, n, h, place, list, total);
   T* out = static_cast<T*>(a.out);
   if (h < 0) {
+    if (blockIdx.x == 0)
+      for (int i = tid; i < n; i += kThreads) report(a, look_up(a, place, a.ids[from + i]));
     if (a.mode == TACG_Q4_SUM) return;
     for (int64_t i = tid; i < static_cast<int64_t>(count) * kWidth; i += kThreads) {
       const int c = column + static_cast<int>(i % kWidth);
@@ -306,111 +370,172 @@ __global__ __launch_bounds__(kThreads) void q4_tiles(Q4Args a) {
     }
     return;
   }
-  int64_t row[RT];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    int v = column + 16 * (GLU ? r % (RT / 2) : r) + (lane & 15);
-    v = v < width ? v : width - 1;
-    row[r] = static_cast<int64_t>(h) * a.N + v + (GLU && r >= RT / 2 ? width : 0);
-  }
-  const int steps = (a.K + kStep - 1) / kStep;
   for (int base = 0; base < count; base += 16 * TT) {
-    const T* x[TT];
+    const T* x[kLoads];
+    uint4v piece[kLoads];
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      const int i = base + 16 * t + (lane & 15);
-      const uint32_t pair = static_cast<uint32_t>(from) + (i < count ? list[i] : 0);
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = base + 8 * i + (tid >> 5);  // past the last token: its values again, for sums that nobody takes
+      const uint32_t pair = static_cast<uint32_t>(from) + list[at < count ? at : count - 1];
       const uint32_t token = pair / a.k, j = pair % a.k;
-      x[t] = i < count ? static_cast<const T*>(a.x) + token * a.x_token + j * a.x_slot : nullptr;
+      x[i] = static_cast<const T*>(a.x) + token * a.x_token + j * a.x_slot;
     }
+    auto fetch = [&](int s) {
+      const bool whole = (s + 1) * kStep <= a.K;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) piece[i] = load_token(a, x[i], s * kStep + 8 * (tid & 31), whole);
+    };
+    auto stage = [&](int s) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        *reinterpret_cast<uint4v*>(&held[s & 1][8 * i + (tid >> 5)][16 * (tid & 31)]) = in_order(piece[i]);
+    };
+    Weights<T, RT, GROUPS> now, next;
+    fetch(0);
+    load_weights(a, 0, quarter, rows, now);
     float4v sum[RT][TT];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
       for (int t = 0; t < TT; ++t) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    if (wave < steps) {
-      Operands<T, RT, TT, PER> now, next;
-      load_step(a, wave, quarter, row, x, now);
-      for (int s = wave; s < steps; s += kWaves) {
-        if (s + kWaves < steps) load_step(a, s + kWaves, quarter, row, x, next);
-        add_step(now, 1.0f, sum);
-        now = next;
+    stage(0);
+    if (steps > 1) fetch(1);
+    __syncthreads();
+    for (int s = 0; s < steps; ++s) {
+      load_weights(a, s + 1 < steps ? s + 1 : s, quarter, rows, next);
+      add_step<T, RT, TT, GROUPS>(now, [&](int t, int i) {
+        return *reinterpret_cast<const uint4v*>(&held[s & 1][16 * t + (lane & 15)][64 * i + 16 * quarter]);
+      }, 1.0f, sum);
+      if (s + 1 < steps) {
+        stage(s + 1);
+        if (s + 2 < steps) fetch(s + 2);
       }
+      __syncthreads();
+      now = next;
     }
+    constexpr int kRows = GLU ? RT / 2 : RT;
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      float4v mine[RT];
+    for (int t = 0; t < TT; ++t)
 #pragma unroll
-      for (int r = 0; r < RT; ++r) mine[r] = sum[r][t];
-      join<RT, kWidth>(red, mine, GLU, [&](int token, int c, float v) {
-        const int i = base + 16 * t + token;
-        if (i >= count || column + c >= width) return;
-        const int64_t at = (from + list[i]) * width + column + c;
-        if (a.mode == TACG_Q4_SUM) a.part[at] = v;
-        else out[at] = static_cast<T>(v);
-      });
-    }
+      for (int j = 0; j < 4; ++j) {
+        const int i = base + 16 * t + 4 * quarter + j;
+        if (i >= count) continue;
+        const int64_t at = (from + list[i]) * width;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          const int c = column + wave * kOut + 16 * r + (lane & 15);
+          if (c >= width) continue;
+          const float v = GLU ? silu(sum[r][t][j]) * sum[r + (GLU ? kRows : 0)][t][j] : sum[r][t][j];
+          if (a.mode == TACG_Q4_SUM) a.part[at + c] = v;
+          else out[at + c] = static_cast<T>(v);
+        }
+      }
   }
 }
 
-// grid: (blocks of 16 RT weight rows, tokens).
-template <class T, int RT, int PER>
-__global__ __launch_bounds__(kThreads) void q4_sum_token(Q4Args a) {
-  __shared__ float red[kWaves][16][RT * 16 + 4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, quarter = lane >> 4;
-  __shared__ int held_at[TACG_MAX_TOPK], slots[TACG_MAX_TOPK], count;
-  const int64_t t = blockIdx.y;
-  if (wave == 0) {  // the served slots, in order
-    int h = -1;
-    if (lane < a.k) {
-      const int id = a.ids[t * a.k + lane];
-      h = static_cast<uint32_t>(id) < static_cast<uint32_t>(a.E) ? place_of(a, id) : id == -1 ? -1 : kBadId;
-      if (blockIdx.x == 0) report(a, h);
+// Few pairs.  The waves of a workgroup share its weight rows and take the steps in turn; their sums are added up in LDS, in order.
+// grid: (blocks of 16 output columns; EACH and GLU: pairs, of which the first of each expert serves all of them, SUM: tokens).
+template <class T, int MODE, int WAVES, int GROUPS>
+__global__ __launch_bounds__(WAVES * 64, 4) void q4_few(Q4Args a) {
+  constexpr bool GLU = MODE == TACG_Q4_GLU, SUM = MODE == TACG_Q4_SUM;
+  constexpr int RT = GLU ? 2 : 1;
+  constexpr int kTokens = SUM ? 1 : 16;
+  __shared__ float red[WAVES][kTokens][RT * 16 + (SUM ? 0 : 4)];
+  __shared__ uint16_t list[TACG_MAX_EXPERTS];
+  __shared__ int16_t place[TACG_MAX_EXPERTS];
+  __shared__ int total[WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int width = GLU ? a.N / 2 : a.N;
+  const int n = blockIdx.x * 16 + (lane & 15), column = n < width ? n : width - 1;
+  const int steps = (a.K + kStep - 1) / kStep;
+  T* out = static_cast<T*>(a.out);
+  int h = -1, count;
+  if constexpr (SUM) {  // list: the token's served slots, place: their matrices
+    if (wave == 0) {
+      int p = -1;
+      if (lane < a.k) {
+        const int id = a.ids[blockIdx.y * a.k + lane];
+        p = static_cast<uint32_t>(id) < static_cast<uint32_t>(a.E) ? place_of(a, id) : id == -1 ? -1 : kBadId;
+        if (blockIdx.x == 0) report(a, p);
+      }
+      const uint64_t some = __ballot(p >= 0);
+      if (p >= 0) {
+        const int at = __popcll(some & ((1ull << lane) - 1));
+        place[at] = static_cast<int16_t>(p);
+        list[at] = static_cast<uint16_t>(lane);
+      }
+      if (lane == 0) total[0] = __popcll(some);
     }
-    const uint64_t some = __ballot(h >= 0);
-    if (h >= 0) {
-      const int at = __popcll(some & ((1ull << lane) - 1));
-      held_at[at] = h;
-      slots[at] = lane;
+    __syncthreads();
+    count = total[0];
+  } else {
+    for (int e = tid; e < a.E; e += WAVES * 64) place[e] = static_cast<int16_t>(place_of(a, e));
+    __syncthreads();
+    h = look_up(a, place, a.ids[blockIdx.y]);
+    if (blockIdx.x == 0 && tid == 0) report(a, h);
+    h = h < 0 ? -1 : h;
+    count = list_pairs<1>(a, 0, static_cast<int>(a.n_tokens * a.k), h, place, list, total);
+    if (list[0] != blockIdx.y) return;
+    if (h < 0) {
+      for (int i = tid; i < 16 * count; i += WAVES * 64)
+        if (blockIdx.x * 16 + i % 16 < width)
+          out[static_cast<int64_t>(list[i / 16]) * width + blockIdx.x * 16 + i % 16] = static_cast<T>(0.0f);
+      return;
     }
-    if (lane == 0) count = __popcll(some);
   }
-  __syncthreads();
-  const int served = count;
-  const int column = blockIdx.x * RT * 16;
-  const int steps = (a.K + kStep - 1) / kStep, items = served * steps;
-  float4v sum[RT][1];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) sum[r][0] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-  Operands<T, RT, 1, PER> now, next;
-  float gate = 0.0f, gate_next = 0.0f;
-  auto load = [&](int i, Operands<T, RT, 1, PER>& o, float& g) {
-    const int j = i / steps;
-    int64_t row[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int v = column + 16 * r + (lane & 15);
-      row[r] = static_cast<int64_t>(held_at[j]) * a.N + (v < a.N ? v : a.N - 1);
+  const int items = SUM ? count * steps : steps;
+  for (int base = 0; base < (SUM ? 1 : count); base += 16) {
+    const T* x = static_cast<const T*>(a.x);
+    if constexpr (!SUM) {  // past the last token: its values again, for sums that nobody takes
+      const uint32_t pair = list[base + (lane & 15) < count ? base + (lane & 15) : count - 1];
+      x += static_cast<int64_t>(pair / a.k) * a.x_token + static_cast<int64_t>(pair % a.k) * a.x_slot;
     }
-    const T* x[1] = {(lane & 15) == 0 ? static_cast<const T*>(a.x) + t * a.x_token + slots[j] * a.x_slot : nullptr};
-    load_step(a, i % steps, quarter, row, x, o);
-    g = a.gate[t * a.k + slots[j]];
-  };
-  if (wave < items) {
-    load(wave, now, gate);
-    for (int i = wave; i < items; i += kWaves) {
-      if (i + kWaves < items) load(i + kWaves, next, gate_next);
-      add_step(now, gate, sum);
-      now = next;
-      gate = gate_next;
+    float4v sum[RT][1];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) sum[r][0] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = wave; i < items; i += WAVES) {
+      int s = i;
+      float factor = 1.0f;
+      const T* token = x;
+      if constexpr (SUM) {
+        const int j = i / steps, slot = __builtin_amdgcn_readfirstlane(list[j]);
+        s = i - j * steps;
+        h = __builtin_amdgcn_readfirstlane(place[j]);
+        factor = a.gate[blockIdx.y * a.k + slot];
+        token += blockIdx.y * a.x_token + slot * a.x_slot;
+      }
+      Rows<T, RT> rows = rows_of<T, RT>(a, h);
+      rows.at[0] = column;
+      if constexpr (GLU) rows.at[1] = column + width;
+      Weights<T, RT, GROUPS> w;
+      load_weights(a, s, quarter, rows, w);
+      uint4v v[kBlocks];
+      const bool whole = (s + 1) * kStep <= a.K;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) v[b] = load_token(a, token, s * kStep + 32 * b + 8 * quarter, whole);
+      add_step<T, RT, 1, GROUPS>(w, [&](int, int b) { return in_order(v[b]); }, factor, sum);
+    }
+    if (base > 0) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (!SUM || (quarter == 0 && j == 0)) red[wave][SUM ? 0 : 4 * quarter + j][16 * r + (lane & 15)] = sum[r][0][j];
+    __syncthreads();
+    for (int i = tid; i < 16 * kTokens; i += WAVES * 64) {
+      const int t = i / 16, c = blockIdx.x * 16 + i % 16;
+      if (c >= width || (!SUM && base + t >= count)) continue;
+      float y = 0.0f, u = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        y += red[w][t][i % 16];
+        if (GLU) u += red[w][t][i % 16 + (GLU ? 16 : 0)];
+      }
+      const int64_t at = SUM ? blockIdx.y : list[base + t];
+      out[at * width + c] = static_cast<T>(GLU ? silu(y) * u : y);
     }
   }
-  float4v mine[RT];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) mine[r] = sum[r][0];
-  join<RT, RT * 16>(red, mine, false, [&](int token, int c, float v) {
-    if (token == 0 && column + c < a.N) static_cast<T*>(a.out)[t * a.N + column + c] = static_cast<T>(v);
-  });
 }
 
 // grid: (blocks of output columns, tokens).
@@ -529,27 +654,37 @@ namespace {
 template <class T, bool GLU, int RT, int TT>
 void start_tiles(const Q4Args& a, hipStream_t stream) {
   const int64_t pairs = a.n_tokens * a.k;
-  const int width = GLU ? a.N / 2 : a.N, block = GLU ? RT * 8 : RT * 16;
-  const dim3 grid((width + block - 1) / block, a.few ? static_cast<uint32_t>(pairs) : a.H + 1,
-                  static_cast<uint32_t>((pairs + kScan - 1) / kScan));
-  if (a.group == 32) q4_tiles<T, GLU, RT, TT, 4><<<grid, kThreads, 0, stream>>>(a);
-  else if (a.group == 64) q4_tiles<T, GLU, RT, TT, 2><<<grid, kThreads, 0, stream>>>(a);
+  const int width = GLU ? a.N / 2 : a.N, block = (GLU ? RT * 8 : RT * 16) * kWaves;
+  const dim3 grid((width + block - 1) / block, a.H + 1, static_cast<uint32_t>((pairs + kScan - 1) / kScan));
+  if (a.group == 32) q4_tiles<T, GLU, RT, TT, 8><<<grid, kThreads, 0, stream>>>(a);
+  else if (a.group == 64) q4_tiles<T, GLU, RT, TT, 4><<<grid, kThreads, 0, stream>>>(a);
+  else if (a.group == 128) q4_tiles<T, GLU, RT, TT, 2><<<grid, kThreads, 0, stream>>>(a);
   else q4_tiles<T, GLU, RT, TT, 1><<<grid, kThreads, 0, stream>>>(a);
+}
+
+template <class T, int MODE, int WAVES>
+void start_few(const Q4Args& a, hipStream_t stream) {
+  const int width = MODE == TACG_Q4_GLU ? a.N / 2 : a.N;
+  const dim3 grid((width + 15) / 16, static_cast<uint32_t>(MODE == TACG_Q4_SUM ? a.n_tokens : a.n_tokens * a.k));
+  if (a.group == 32) q4_few<T, MODE, WAVES, 8><<<grid, WAVES * 64, 0, stream>>>(a);
+  else if (a.group == 64) q4_few<T, MODE, WAVES, 4><<<grid, WAVES * 64, 0, stream>>>(a);
+  else if (a.group == 128) q4_few<T, MODE, WAVES, 2><<<grid, WAVES * 64, 0, stream>>>(a);
+  else q4_few<T, MODE, WAVES, 1><<<grid, WAVES * 64, 0, stream>>>(a);
 }
 
 template <class T>
 void start(const Q4Args& a, hipStream_t stream) {
-  if (a.few && a.mode == TACG_Q4_SUM) {
-    const dim3 grid((a.N + 15) / 16, static_cast<uint32_t>(a.n_tokens));
-    if (a.group == 32) q4_sum_token<T, 1, 4><<<grid, kThreads, 0, stream>>>(a);
-    else if (a.group == 64) q4_sum_token<T, 1, 2><<<grid, kThreads, 0, stream>>>(a);
-    else q4_sum_token<T, 1, 1><<<grid, kThreads, 0, stream>>>(a);
+  const int64_t pairs = a.n_tokens * a.k;
+  const bool glu = a.mode == TACG_Q4_GLU;
+  if (few_pairs(pairs, a.E)) {
+    if (a.mode == TACG_Q4_SUM) start_few<T, TACG_Q4_SUM, 16>(a, stream);
+    else if (glu) start_few<T, TACG_Q4_GLU, 8>(a, stream);
+    else start_few<T, TACG_Q4_EACH, 8>(a, stream);
     return;
   }
-  const bool glu = a.mode == TACG_Q4_GLU;
-  const bool two = !a.few && a.n_tokens * a.k > 10 * static_cast<int64_t>(a.E);
-  if (glu) two ? start_tiles<T, true, 4, 2>(a, stream) : start_tiles<T, true, 2, 1>(a, stream);
-  else two ? start_tiles<T, false, 4, 2>(a, stream) : start_tiles<T, false, 2, 1>(a, stream);
+  const bool two = pairs > 10 * static_cast<int64_t>(a.E);
+  if (glu) two ? start_tiles<T, true, 2, 2>(a, stream) : start_tiles<T, true, 2, 1>(a, stream);
+  else two ? start_tiles<T, false, 2, 2>(a, stream) : start_tiles<T, false, 2, 1>(a, stream);
   if (a.mode == TACG_Q4_SUM)
     q4_combine<T><<<dim3((a.N + 255) / 256, static_cast<uint32_t>(std::min<int64_t>(a.n_tokens, 65535))), 256, 0, stream>>>(a);
 }
@@ -583,7 +718,6 @@ int launch_expert_q4(const void* x, int32_t dtype, int64_t x_stride_token, int64
   a.gate = gate;
   a.out = out;
   a.err = d_err;
-  a.few = few_pairs(n_tokens * top_k, n_experts);
   a.part = static_cast<float*>(workspace);
   if (dtype == TACG_BF16) start<__bf16>(a, stream);
   else start<_Float16>(a, stream);

@@ -20,6 +20,7 @@
 // q4_combine: sums the 32-bit products of many pairs over the slots of a token.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "tacg_internal.h"
 
@@ -105,12 +106,13 @@ struct Rows {
   uint32_t at[RT];  // row
 };
 
-// A step's weights of a lane, as loaded.  GROUPS: scale groups of a step, two scales and four zeros to a word.
-template <class T, int RT, int GROUPS>
+// A step's weights of a lane, as loaded.  GROUPS: scale groups of a step, two scales and four zeros to a word.  ZEROS: whether zeros are
+// given (a choice at run time would merge two values after their load, and so wait for it there).
+template <class T, int RT, int GROUPS, bool ZEROS>
 struct Weights {
   uint4v level[RT][2];
   uint32_t scale[RT][(GROUPS + 1) / 2];
-  uint32_t zero[RT][(GROUPS + 3) / 4];
+  uint32_t zero[ZEROS ? RT : 1][(GROUPS + 3) / 4];
 };
 
 template <class T, int RT>
@@ -124,10 +126,18 @@ __device__ __forceinline__ Rows<T, RT> rows_of(const Q4Args& a, int h) {
 }
 
 // The words of N values of a row's groups from `first` on; past the row's end any that can be read safely (the tokens' values are 0 there).
-template <int N, class V, int W>
+// WHOLE: none lies past it.
+template <int N, bool WHOLE, class V, int W>
 __device__ __forceinline__ void load_groups(const V* row, int first, int n_groups, uint32_t (&o)[W]) {
   constexpr int kBits = 8 * sizeof(V);
-  if (n_groups >= N) {
+  if constexpr (WHOLE) {
+    if constexpr (N * sizeof(V) < 4) {
+      o[0] = 0;
+      __builtin_memcpy(o, row + first, N * sizeof(V));
+    } else {
+      __builtin_memcpy(o, row + first, sizeof(o));
+    }
+  } else if (n_groups >= N) {
     const int from = first + N <= n_groups ? first : n_groups - N, skip = (first - from) * kBits;
     if constexpr (N * sizeof(V) < 4) {
       o[0] = 0;
@@ -161,34 +171,30 @@ __device__ __forceinline__ void load_groups(const V* row, int first, int n_group
   }
 }
 
-template <class T, int RT, int GROUPS>
+// WHOLE: the step ends before the columns do.  A choice at run time would make the compiler wait for the fewest loads that either way issues.
+template <bool WHOLE, class T, int RT, int GROUPS, bool ZEROS>
 __device__ __forceinline__ void load_weights(const Q4Args& a, int s, int quarter, const Rows<T, RT>& rows,
-                                             Weights<T, RT, GROUPS>& o) {
+                                             Weights<T, RT, GROUPS, ZEROS>& o) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     int piece = 8 * s + 4 * i + quarter;  // past the end the tokens' values are 0: any levels do
-    piece = piece < a.pieces ? piece : a.pieces - 1;
+    if (!WHOLE) piece = piece < a.pieces ? piece : a.pieces - 1;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
       o.level[r][i] = *reinterpret_cast<const uint4v*>(rows.level + 16u * (rows.at[r] * a.pieces + piece));
   }
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    load_groups<GROUPS>(rows.scale + rows.at[r] * a.n_groups, s * GROUPS, a.n_groups, o.scale[r]);
-    if (a.zeros != nullptr) {
-      load_groups<GROUPS>(rows.zero + rows.at[r] * a.n_groups, s * GROUPS, a.n_groups, o.zero[r]);
-    } else {
-#pragma unroll
-      for (int w = 0; w < (GROUPS + 3) / 4; ++w) o.zero[r][w] = 0x08080808u;
-    }
+    load_groups<GROUPS, WHOLE>(rows.scale + rows.at[r] * a.n_groups, s * GROUPS, a.n_groups, o.scale[r]);
+    if constexpr (ZEROS) load_groups<GROUPS, WHOLE>(rows.zero + rows.at[r] * a.n_groups, s * GROUPS, a.n_groups, o.zero[r]);
   }
 }
 
-// Eight values of a token from column c on, 0 past the columns' end; `whole`: the step has no end in it.
-template <class T>
-__device__ __forceinline__ uint4v load_token(const Q4Args& a, const T* x, int c, bool whole) {
+// Eight values of a token from column c on, 0 past the columns' end.
+template <bool WHOLE, class T>
+__device__ __forceinline__ uint4v load_token(const Q4Args& a, const T* x, int c) {
   uint4v o = {0, 0, 0, 0};
-  if (whole || c + 8 <= a.K) {
+  if (WHOLE || c + 8 <= a.K) {
     __builtin_memcpy(&o, x + c, 16);  // rows need not be aligned to more than an element
   } else if (c < a.K) {
 #pragma unroll
@@ -213,8 +219,8 @@ __device__ __forceinline__ float half_of(uint32_t word, int i) {
 }
 
 // sum += factor * scale * (level - zero) . x of one step; tokens(t, i): the lane's ordered values of block i of token tile t.
-template <class T, int RT, int TT, int GROUPS, class Tokens>
-__device__ __forceinline__ void add_step(const Weights<T, RT, GROUPS>& o, Tokens tokens, float factor,
+template <class T, int RT, int TT, int GROUPS, bool ZEROS, class Tokens>
+__device__ __forceinline__ void add_step(const Weights<T, RT, GROUPS, ZEROS>& o, Tokens tokens, float factor,
                                          float4v (&sum)[RT][TT]) {
   constexpr int kRun = kBlocks / GROUPS;  // products of a group
   constexpr uint32_t kOnes = __is_same(T, __bf16) ? 0x3f803f80u : 0x3c003c00u;
@@ -260,7 +266,7 @@ __device__ __forceinline__ void add_step(const Weights<T, RT, GROUPS>& o, Tokens
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const float scale = half_of<T>(o.scale[r][g / 2], g % 2) * factor;
-      const float zero = kOffset<T> + static_cast<float>((o.zero[r][g / 4] >> (8 * (g % 4))) & 255u);
+      const float zero = kOffset<T> + (ZEROS ? static_cast<float>((o.zero[ZEROS ? r : 0][g / 4] >> (8 * (g % 4))) & 255u) : 8.0f);
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
 #pragma unroll
@@ -331,7 +337,7 @@ constexpr int kTokenBytes = kStep * 2 + 16;  // of a token's step in LDS: 16 tok
 
 // Many pairs.  grid: (blocks of a workgroup's output columns, held experts and one for the pairs that none serves, runs of kScan pairs).
 // Every wave has weight rows of its own; the tokens' values come through LDS, a step ahead, in two buffers.
-template <class T, bool GLU, int RT, int TT, int GROUPS>
+template <class T, bool GLU, int RT, int TT, int GROUPS, bool ZEROS>
 __global__ __launch_bounds__(kThreads, 2) void q4_tiles(Q4Args a) {
   constexpr int kOut = GLU ? RT * 8 : RT * 16;  // output columns of a wave
   constexpr int kWidth = kOut * kWaves;         // of the workgroup
@@ -348,7 +354,6 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tiles(Q4Args a) {
   const int h = static_cast<int>(blockIdx.y) < a.H ? static_cast<int>(blockIdx.y) : -1;
   const int column = blockIdx.x * kWidth;
   const int width = GLU ? a.N / 2 : a.N;
-  const int steps = (a.K + kStep - 1) / kStep;
   Rows<T, RT> rows = rows_of<T, RT>(a, h);
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -380,39 +385,51 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tiles(Q4Args a) {
       const uint32_t token = pair / a.k, j = pair % a.k;
       x[i] = static_cast<const T*>(a.x) + token * a.x_token + j * a.x_slot;
     }
-    auto fetch = [&](int s) {
-      const bool whole = (s + 1) * kStep <= a.K;
+    auto fetch = [&](auto whole, int s) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) piece[i] = load_token(a, x[i], s * kStep + 8 * (tid & 31), whole);
+      for (int i = 0; i < kLoads; ++i) piece[i] = load_token<whole.value>(a, x[i], s * kStep + 8 * (tid & 31));
     };
     auto stage = [&](int s) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         *reinterpret_cast<uint4v*>(&held[s & 1][8 * i + (tid >> 5)][16 * (tid & 31)]) = in_order(piece[i]);
     };
-    Weights<T, RT, GROUPS> now, next;
-    fetch(0);
-    load_weights(a, 0, quarter, rows, now);
     float4v sum[RT][TT];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
       for (int t = 0; t < TT; ++t) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    stage(0);
-    if (steps > 1) fetch(1);
-    __syncthreads();
-    for (int s = 0; s < steps; ++s) {
-      load_weights(a, s + 1 < steps ? s + 1 : s, quarter, rows, next);
-      add_step<T, RT, TT, GROUPS>(now, [&](int t, int i) {
+    Weights<T, RT, GROUPS, ZEROS> now, next;
+    auto add = [&](int s) {
+      add_step<T, RT, TT, GROUPS, ZEROS>(now, [&](int t, int i) {
         return *reinterpret_cast<const uint4v*>(&held[s & 1][16 * t + (lane & 15)][64 * i + 16 * quarter]);
       }, 1.0f, sum);
-      if (s + 1 < steps) {
-        stage(s + 1);
-        if (s + 2 < steps) fetch(s + 2);
-      }
+    };
+    const std::true_type whole;
+    const int last = a.K / kStep - 1;  // of the steps before the columns' end
+    if (last >= 0) {
+      fetch(whole, 0);
+      load_weights<true>(a, 0, quarter, rows, now);
+      stage(0);
+      fetch(whole, last < 1 ? last : 1);
+    }
+    __syncthreads();
+    for (int s = 0; s <= last; ++s) {  // what is brought after the last step is not used
+      load_weights<true>(a, s < last ? s + 1 : last, quarter, rows, next);
+      add(s);
+      stage(s + 1);
+      fetch(whole, s + 2 <= last ? s + 2 : last);
       __syncthreads();
       now = next;
     }
+    if ((last + 1) * kStep < a.K) {
+      fetch(std::false_type(), last + 1);
+      load_weights<false>(a, last + 1, quarter, rows, now);
+      stage(last + 1);
+      __syncthreads();
+      add(last + 1);
+    }
+    __syncthreads();  // the buffers are free for the next tokens
     constexpr int kRows = GLU ? RT / 2 : RT;
 #pragma unroll
     for (int t = 0; t < TT; ++t)
@@ -435,7 +452,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tiles(Q4Args a) {
 
 // Few pairs.  The waves of a workgroup share its weight rows and take the steps in turn; their sums are added up in LDS, in order.
 // grid: (blocks of 16 output columns; EACH and GLU: pairs, of which the first of each expert serves all of them, SUM: tokens).
-template <class T, int MODE, int WAVES, int GROUPS>
+template <class T, int MODE, int WAVES, int GROUPS, bool ZEROS>
 __global__ __launch_bounds__(WAVES * 64, 4) void q4_few(Q4Args a) {
   constexpr bool GLU = MODE == TACG_Q4_GLU, SUM = MODE == TACG_Q4_SUM;
   constexpr int RT = GLU ? 2 : 1;
@@ -508,13 +525,16 @@ __global__ __launch_bounds__(WAVES * 64, 4) void q4_few(Q4Args a) {
       Rows<T, RT> rows = rows_of<T, RT>(a, h);
       rows.at[0] = column;
       if constexpr (GLU) rows.at[1] = column + width;
-      Weights<T, RT, GROUPS> w;
-      load_weights(a, s, quarter, rows, w);
+      Weights<T, RT, GROUPS, ZEROS> w;
       uint4v v[kBlocks];
-      const bool whole = (s + 1) * kStep <= a.K;
+      auto load = [&](auto whole) {
+        load_weights<whole.value>(a, s, quarter, rows, w);
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) v[b] = load_token(a, token, s * kStep + 32 * b + 8 * quarter, whole);
-      add_step<T, RT, 1, GROUPS>(w, [&](int, int b) { return in_order(v[b]); }, factor, sum);
+        for (int b = 0; b < kBlocks; ++b) v[b] = load_token<whole.value>(a, token, s * kStep + 32 * b + 8 * quarter);
+      };
+      if ((s + 1) * kStep <= a.K) load(std::true_type());
+      else load(std::false_type());
+      add_step<T, RT, 1, GROUPS, ZEROS>(w, [&](int, int b) { return in_order(v[b]); }, factor, sum);
     }
     if (base > 0) __syncthreads();
 #pragma unroll
@@ -651,25 +671,36 @@ size_t expert_q4_workspace(int64_t n_tokens, int32_t top_k, int32_t n_experts, i
 
 namespace {
 
+// launch(groups of a step, whether zeros are given)
+template <class Launch>
+void by_weights(const Q4Args& a, Launch launch) {
+  auto with = [&](auto groups) {
+    if (a.zeros != nullptr) launch(groups, std::true_type());
+    else launch(groups, std::false_type());
+  };
+  if (a.group == 32) with(std::integral_constant<int, 8>());
+  else if (a.group == 64) with(std::integral_constant<int, 4>());
+  else if (a.group == 128) with(std::integral_constant<int, 2>());
+  else with(std::integral_constant<int, 1>());
+}
+
 template <class T, bool GLU, int RT, int TT>
 void start_tiles(const Q4Args& a, hipStream_t stream) {
   const int64_t pairs = a.n_tokens * a.k;
   const int width = GLU ? a.N / 2 : a.N, block = (GLU ? RT * 8 : RT * 16) * kWaves;
   const dim3 grid((width + block - 1) / block, a.H + 1, static_cast<uint32_t>((pairs + kScan - 1) / kScan));
-  if (a.group == 32) q4_tiles<T, GLU, RT, TT, 8><<<grid, kThreads, 0, stream>>>(a);
-  else if (a.group == 64) q4_tiles<T, GLU, RT, TT, 4><<<grid, kThreads, 0, stream>>>(a);
-  else if (a.group == 128) q4_tiles<T, GLU, RT, TT, 2><<<grid, kThreads, 0, stream>>>(a);
-  else q4_tiles<T, GLU, RT, TT, 1><<<grid, kThreads, 0, stream>>>(a);
+  by_weights(a, [&](auto groups, auto zeros) {
+    q4_tiles<T, GLU, RT, TT, groups.value, zeros.value><<<grid, kThreads, 0, stream>>>(a);
+  });
 }
 
 template <class T, int MODE, int WAVES>
 void start_few(const Q4Args& a, hipStream_t stream) {
   const int width = MODE == TACG_Q4_GLU ? a.N / 2 : a.N;
   const dim3 grid((width + 15) / 16, static_cast<uint32_t>(MODE == TACG_Q4_SUM ? a.n_tokens : a.n_tokens * a.k));
-  if (a.group == 32) q4_few<T, MODE, WAVES, 8><<<grid, WAVES * 64, 0, stream>>>(a);
-  else if (a.group == 64) q4_few<T, MODE, WAVES, 4><<<grid, WAVES * 64, 0, stream>>>(a);
-  else if (a.group == 128) q4_few<T, MODE, WAVES, 2><<<grid, WAVES * 64, 0, stream>>>(a);
-  else q4_few<T, MODE, WAVES, 1><<<grid, WAVES * 64, 0, stream>>>(a);
+  by_weights(a, [&](auto groups, auto zeros) {
+    q4_few<T, MODE, WAVES, groups.value, zeros.value><<<grid, WAVES * 64, 0, stream>>>(a);
+  });
 }
 
 template <class T>

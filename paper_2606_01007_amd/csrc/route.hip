@@ -6,13 +6,21 @@
 // s' = s (softmax) or s / sum s (sigmoid), a segment of T rows with D_e selections and M_e = sum_t s'_e(t) has
 //   balance = E / (k T^2) sum_e D_e M_e,   z = 1/T sum_t lse_t^2.
 //
-// route_main: one pass over the logits.  A workgroup takes a run of rows of one segment; its sums of s' (32 bits over a run, then 64),
-//   counts, rows and squares go to a slot of the workspace, and route_reduce adds a segment's slots in order in 64 bits, so
-//   that results do not depend on the order of execution.
+// route_main: one pass over the logits.  Selection in a row:
+//   * a lane's elements fall into up to eight groups; the k-th largest (8th or 16th, by the kernel's variant) of the row's group maxima,
+//     found by sorting networks within and merges across the lanes, is a lower bound of the k-th largest logit that few more than k
+//     elements reach;
+//   * those elements' values, with the id below the value's last bit (32-bit value and id in a 64-bit float), go to a list in LDS;
+//   * the place of each is the number of larger ones in the list.
+//   A row with more than kList such elements (many equal ones) is selected by k passes over the registers instead.
+//   A workgroup takes a run of rows of one segment; its sums of s' (32 bits over a run, then 64), counts, rows and squares go to a
+//   slot of the workspace, and route_reduce adds a segment's slots in order in 64 bits, so that results do not depend on the
+//   order of execution.
 // route_back: one pass over logits and gradient; with c = d loss / d s' (a constant of the
 //   segment) and u the gradient of the scores through the gates, softmax: dx = s (c + u - sum s (c + u) + 2 gz lse / T).
 //   u has k entries a row: they are laid into a row of LDS, where each lane reads its own experts' back.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "tacg_internal.h"
@@ -131,18 +139,135 @@ __device__ __forceinline__ void store_row(T* row, int sub, int E, int vec, const
   }
 }
 
-__device__ __forceinline__ float row_max(float v) {
-#pragma unroll
-  for (int o = 1; o < kRowLanes; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+// Exchanges within the eight lanes of a row: with the lane whose number differs in bit 0, in bit 1, in all three.
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror = 0x141;
+template <int CTRL>
+__device__ __forceinline__ int across(int v) {
+  return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true);
 }
-__device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-  for (int o = 1; o < kRowLanes; o <<= 1) v += __shfl_xor(v, o, 64);
-  return v;
+template <int CTRL>
+__device__ __forceinline__ float across(float v) {
+  return __int_as_float(across<CTRL>(__float_as_int(v)));
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
+// The instructions themselves: what they return for a NaN does not matter here, and fmaxf() first quiets every operand.
+__device__ __forceinline__ float vmax(float a, float b) {
+  float o;
+  asm("v_max_f32 %0, %1, %2" : "=v"(o) : "v"(a), "v"(b));
+  return o;
+}
+__device__ __forceinline__ float vmin(float a, float b) {
+  float o;
+  asm("v_min_f32 %0, %1, %2" : "=v"(o) : "v"(a), "v"(b));
+  return o;
+}
+__device__ __forceinline__ float vmax3(float a, float b, float c) {
+  float o;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(o) : "v"(a), "v"(b), "v"(c));
+  return o;
+}
+
+__device__ __forceinline__ float row_max(float v) {
+  v = vmax(v, across<kSwap1>(v));
+  v = vmax(v, across<kSwap2>(v));
+  return vmax(v, across<kMirror>(v));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += across<kSwap1>(v);
+  v += across<kSwap2>(v);
+  return v + across<kMirror>(v);
+}
+
+// v_rcp_f32 is within one unit in the last place; an exact division would cost ten instructions.
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
+
+__device__ __forceinline__ void order(float& a, float& b) {  // the larger one first
+  const float hi = vmax(a, b);
+  b = vmin(a, b);
+  a = hi;
+}
+// Sorts a sequence that rises and then falls (or the other way), largest first.
+template <int N>
+__device__ __forceinline__ void sort_bitonic(float* a) {
+  if constexpr (N > 1) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) order(a[i], a[i + N / 2]);
+    sort_bitonic<N / 2>(a);
+    sort_bitonic<N / 2>(a + N / 2);
+  }
+}
+template <int N>
+__device__ __forceinline__ void sort_all(float* a) {
+  if constexpr (N > 1) {
+    sort_all<N / 2>(a);
+    sort_all<N / 2>(a + N / 2);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) order(a[i], a[N - 1 - i]);
+    sort_bitonic<N / 2>(a);
+    sort_bitonic<N / 2>(a + N / 2);
+  }
+}
+// The N largest of the sorted lists of this lane and another; sorted again, or (LAST) only the smallest of them.
+template <int N, int CTRL, bool LAST>
+__device__ __forceinline__ float merge(float (&a)[N]) {
+  float b[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) b[i] = vmax(a[i], across<CTRL>(a[N - 1 - i]));
+  float low = b[0];
+  if constexpr (LAST) {
+#pragma unroll
+    for (int i = 1; i < N; ++i) low = vmin(low, b[i]);
+  } else {
+    sort_bitonic<N>(b);
+#pragma unroll
+    for (int i = 0; i < N; ++i) a[i] = b[i];
+  }
+  return low;
+}
+
+// The KL-th largest of the maxima of the row's groups (-inf if there are fewer), and the largest.  Group j of a lane: elements
+// j, j + G, j + 2 G, ...: neighbouring experts lie in different ones.
+template <int KL, int M>
+__device__ __forceinline__ float lower_bound(const float (&y)[M], float& top) {
+  constexpr int G = M < 8 ? M : 8;
+  float a[KL];
+#pragma unroll
+  for (int i = 0; i < KL; ++i) a[i] = kNone;
+#pragma unroll
+  for (int j = 0; j < G; ++j) {
+    if constexpr (M / G == 4) a[j] = vmax(vmax3(y[j], y[j + G], y[j + 2 * G]), y[j + 3 * G]);
+    else if constexpr (M / G == 2) a[j] = vmax(y[j], y[j + G]);
+    else a[j] = y[j];
+  }
+  sort_all<G>(a);
+  merge<KL, kSwap1, false>(a);
+  merge<KL, kSwap2, false>(a);
+  top = vmax(a[0], across<kMirror>(a[0]));
+  return merge<KL, kMirror, true>(a);
+}
+
+// Bit M - 1 - i of the mask: y[i] >= bound.
+template <int M>
+__device__ __forceinline__ uint32_t at_least(const float (&y)[M], float bound) {
+  uint32_t mask = 0;
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+    asm("v_cmp_ge_f32 vcc, %1, %2\n\tv_addc_co_u32 %0, vcc, %0, %0, vcc" : "+v"(mask) : "v"(y[i]), "v"(bound) : "vcc");
+  return mask;
+}
+
+constexpr int kList = 32;  // elements of a row's list
+
+// A list entry: orders by value, equal values by id, the lower one first.
+__device__ __forceinline__ double entry_of(float v, int e) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, static_cast<double>(v + 0.0f));  // -0 and +0 are equal
+  return __builtin_bit_cast(double, bits | static_cast<uint32_t>(v < 0.0f ? e : 255 - e));
+}
+__device__ __forceinline__ int id_of(double entry) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, entry);
+  const int e = static_cast<int>(bits & 255u);
+  return (bits >> 63) != 0 ? e : 255 - e;
+}
 
 struct Run {
   int family;
@@ -160,10 +285,17 @@ __device__ __forceinline__ Run run_of(const Args& a, int run) {
   return r;
 }
 
-// grid: (runs, layers).  KS: slots that a lane of a row takes (ids sub and sub + 8).
-template <class T, int CH, int KS, bool BAL>
-__global__ __launch_bounds__(kRouteThreads) void route_main(RouteArgs a) {
-  constexpr int V = kChunk<T>, M = CH * V;
+template <class T, int CH>
+__device__ __forceinline__ int element(int i, int sub) {  // the id of a lane's i-th element
+  return ((i / kChunk<T>) * kRowLanes + sub) * kChunk<T> + i % kChunk<T>;
+}
+
+// grid: (runs, layers).  KL: 8 for k <= 8, else 16.
+template <class T, int CH, int KL, bool BAL, bool BIAS>
+__global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
+  constexpr int V = kChunk<T>, M = CH * V, KS = KL / kRowLanes;
+  __shared__ double list[kRowsPerPass][kList];
+  __shared__ int chosen[kRowsPerPass][KL];
   __shared__ uint32_t count[BAL ? TACG_MAX_EXPERTS : 1];
   __shared__ float mass[BAL ? kRouteWaves : 1][BAL ? TACG_MAX_EXPERTS : 1];
   __shared__ float squares[kRouteWaves];
@@ -173,15 +305,20 @@ __global__ __launch_bounds__(kRouteThreads) void route_main(RouteArgs a) {
   const Run run = run_of(a, blockIdx.x);
   const int E = a.E, k = a.k;
   const T* layer = static_cast<const T*>(a.logits) + l * a.stride_layer;
+  double* mine = list[tid >> 3];
+  int* slots = chosen[tid >> 3];
   float acc[BAL ? M : 1];
   float sq = 0.0f;
   uint32_t live = 0;
+  for (int i = sub; i < kList; i += kRowLanes) mine[i] = -INFINITY;
   if (BAL) {
 #pragma unroll
     for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] = 0.0f;
     for (int e = tid; e < E; e += kRouteThreads) count[e] = 0;
     __syncthreads();
   }
+  // whether the sum over all experts is needed
+  const bool all = BAL || BIAS || a.norm != nullptr || (a.softmax && !a.renorm);
   for (int64_t base = run.first; base < run.last; base += kRowsPerPass) {
     const int64_t t = base + (tid >> 3);
     const bool in = t < run.last;
@@ -190,73 +327,137 @@ __global__ __launch_bounds__(kRouteThreads) void route_main(RouteArgs a) {
     load_row<T, CH>(row, sub, E, a.vec, x);
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < M; ++i) bad |= !(x[i] < INFINITY);
+    for (int i = 0; i < M; i += 2) bad |= __builtin_isunordered(x[i], x[i + 1]);
+    float top, bound = 0.0f;
+    if constexpr (BIAS) {
+      top = x[0];
+#pragma unroll
+      for (int i = 1; i < M; ++i) top = vmax(top, x[i]);
+      top = row_max(top);
+    } else {
+      bound = lower_bound<KL>(x, top);
+    }
+    bad |= top == INFINITY;
     if (__any(bad)) {  // a NaN or +inf: the row is not routed
       const uint64_t m = __ballot(bad) >> (lane & ~(kRowLanes - 1));
       if ((m & 0xff) != 0) {
         if (in && sub == 0) atomicOr(a.err, TACG_ERR_VALUE);
+        top = bound = kNone;
 #pragma unroll
         for (int i = 0; i < M; ++i) x[i] = kNone;
       }
     }
-    // scores: p = exp(x - max) (softmax, to be divided by their sum) or the sigmoid
-    float top = kNone, total = 0.0f, p[M];
-    if (a.softmax) {
+    const bool some = top > kNone;
+    uint32_t mask = 0;
+    if constexpr (!BIAS) mask = at_least(x, vmax(bound, -FLT_MAX));
+    // scores: exp(x - top) (softmax, to be divided by their sum) or the sigmoid, in place of the logits
+    const float shift = some ? top : 0.0f;
+    float total = 0.0f, inverse = 0.0f;
+    if (all) {
+      uint32_t away = 0;  // BIAS: which logits are -inf
+      if constexpr (BIAS) away = ~at_least(x, -FLT_MAX);
+      if (a.softmax) {
 #pragma unroll
-      for (int i = 0; i < M; ++i) top = fmaxf(top, x[i]);
-      top = row_max(top);
-    }
-    const float shift = top == kNone ? 0.0f : top;
+        for (int i = 0; i < M; ++i) x[i] = __expf(x[i] - shift), total += x[i];
+      } else {
 #pragma unroll
-    for (int i = 0; i < M; ++i) {
-      p[i] = a.softmax ? __expf(x[i] - shift) : sigmoid(x[i]);
-      total += p[i];
-    }
-    total = row_sum(total);
-    const float inverse = total > 0.0f ? 1.0f / total : 0.0f;
-    // selection: by the logit itself, which orders as its score, or by score + bias
-    float y[M];
+        for (int i = 0; i < M; ++i) x[i] = sigmoid(x[i]), total += x[i];
+      }
+      total = row_sum(total);
+      inverse = total > 0.0f ? 1.0f / total : 0.0f;
+      if (BAL && in) {
 #pragma unroll
-    for (int i = 0; i < M; ++i) y[i] = x[i] + 0.0f;  // -0 and +0 are equal
-    if (a.bias != nullptr) {
+        for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] += x[i] * inverse;
+      }
+      if constexpr (BIAS) {
+        const float f = a.softmax ? inverse : 1.0f;
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const int e = (c * kRowLanes + sub) * V + j, i = c * V + j;
-          const float s = a.softmax ? p[i] * inverse : p[i];
-          y[i] = x[i] > kNone ? s + a.bias[l * E + (e < E ? e : 0)] : kNone;
+        for (int i = 0; i < M; ++i) {
+          const int e = element<T, CH>(i, sub);
+          x[i] = (away >> (M - 1 - i)) & 1u ? kNone : x[i] * f + a.bias[l * E + (e < E ? e : 0)];
         }
+        float unused;
+        bound = lower_bound<KL>(x, unused);
+        mask = at_least(x, vmax(bound, -FLT_MAX));
+      }
     }
-    int id[KS];
+    // what the selection orders by, of one expert
+    auto value = [&](int e) {
+      float v = widen(row[e]);
+      if constexpr (BIAS) v = (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e];
+      return v;
+    };
+    // the list: each lane's elements after those of the lanes before it
+    int n = __popc(mask), before = 0;
+    {
+      int o = across<kSwap1>(n);
+      before += sub & 1 ? o : 0;
+      n += o;
+      o = across<kSwap2>(n);
+      before += sub & 2 ? o : 0;
+      n += o;
+      o = across<kMirror>(n);
+      before += sub & 4 ? o : 0;
+      n += o;
+    }
+    int most = 0;  // of the wave's rows
+#pragma unroll
+    for (int r = 0; r < 64; r += kRowLanes) {
+      const int v = __builtin_amdgcn_readlane(n, r);
+      most = v > most ? v : most;
+    }
+    int id[KS];  // of slots sub, sub + 8
 #pragma unroll
     for (int q = 0; q < KS; ++q) id[q] = -1;
-    float last = INFINITY;
-    int last_e = -1;
-    for (int j = 0; j < k; ++j) {  // the best after the last winner in (value descending, id ascending)
-      float best = kNone;
-      int at = 0x7fffffff;
+    if (most <= kList) {
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
+      for (int q = 0; q < KS; ++q) slots[sub + q * kRowLanes] = -1;
+      while (__any(mask != 0)) {
+        if (mask != 0) {
+          const int i = __clz(mask) - (32 - M);
+          mask &= ~(1u << (M - 1 - i));
+          const int e = element<T, CH>(i, sub);
+          mine[before++] = entry_of(value(e), e);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      for (int first = 0; first < most; first += kRowLanes) {
+        const double own = mine[first + sub];
+        int larger = 0;
+        for (int i = 0; i < most; ++i) larger += mine[i] > own;
+        if (first + sub < n && larger < k) slots[larger] = id_of(own);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int q = 0; q < V; ++q) {
-          const int e = (c * kRowLanes + sub) * V + q;
-          const float v = y[c * V + q];
+      for (int q = 0; q < KS; ++q) id[q] = slots[sub + q * kRowLanes];
+      for (int i = sub; i < most; i += kRowLanes) mine[i] = -INFINITY;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    } else {
+      // k passes: the best after the last winner in (value descending, id ascending).  The values are read again.
+      float last = INFINITY;
+      int last_e = -1;
+      for (int j = 0; j < k; ++j) {
+        float best = kNone;
+        int at = 0x7fffffff;
+        for (int i = 0; i < M; ++i) {
+          const int e = element<T, CH>(i, sub);
+          if (e >= E || !some) continue;
+          const float v = widen(row[e]) > kNone ? value(e) : kNone;
           const bool after = v < last || (v == last && e > last_e);
           if (after && v > best) best = v, at = e;
         }
 #pragma unroll
-      for (int o = 1; o < kRowLanes; o <<= 1) {
-        const float v = __shfl_xor(best, o, 64);
-        const int e = __shfl_xor(at, o, 64);
-        if (v > best || (v == best && e < at)) best = v, at = e;
-      }
-      const int winner = best > kNone ? at : -1;
+        for (int o = 1; o < kRowLanes; o <<= 1) {
+          const float v = __shfl_xor(best, o, 64);
+          const int e = __shfl_xor(at, o, 64);
+          if (v > best || (v == best && e < at)) best = v, at = e;
+        }
 #pragma unroll
-      for (int q = 0; q < KS; ++q)
-        if (j == sub + q * kRowLanes) id[q] = winner;
-      last = best > kNone ? best : kNone;
-      last_e = best > kNone ? at : 0x7fffffff;
+        for (int q = 0; q < KS; ++q)
+          if (j == sub + q * kRowLanes && best > kNone) id[q] = at;
+        last = best;
+        last_e = best > kNone ? at : 0x7fffffff;
+      }
     }
     // gates of the selected
     float w[KS];
@@ -264,10 +465,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_main(RouteArgs a) {
     for (int q = 0; q < KS; ++q) w[q] = id[q] >= 0 ? widen(row[id[q]]) : kNone;
     if (a.softmax) {
       float high = shift;
-      if (a.renorm) {
+      if (BIAS && a.renorm) {
         high = kNone;
 #pragma unroll
-        for (int q = 0; q < KS; ++q) high = fmaxf(high, w[q]);
+        for (int q = 0; q < KS; ++q) high = vmax(high, w[q]);
         high = row_max(high);
         high = high == kNone ? 0.0f : high;
       }
@@ -288,22 +489,21 @@ __global__ __launch_bounds__(kRouteThreads) void route_main(RouteArgs a) {
       factor = a.scale * inverse;
     }
     const int64_t at = static_cast<int64_t>(l) * a.n_tokens + t;
+    if (in) {
 #pragma unroll
-    for (int q = 0; q < KS; ++q) {
-      const int j = sub + q * kRowLanes;
-      if (in && j < k) {
-        a.trace[at * k + j] = static_cast<int16_t>(id[q]);
-        a.gate[at * k + j] = w[q] * factor;
-        if (BAL && id[q] >= 0) atomicAdd(&count[id[q]], 1u);
+      for (int q = 0; q < KS; ++q) {
+        const int j = sub + q * kRowLanes;
+        if (j < k) {
+          a.trace[at * k + j] = static_cast<int16_t>(id[q]);
+          a.gate[at * k + j] = w[q] * factor;
+          if (BAL && id[q] >= 0) atomicAdd(&count[id[q]], 1u);
+        }
       }
     }
-    const bool some = __shfl(id[0], lane & ~(kRowLanes - 1), 64) >= 0;
-    const float norm = a.softmax ? (some ? top + __logf(total) : kNone) : total;
-    if (a.norm != nullptr && in && sub == 0) a.norm[at] = norm;
-    if (BAL && in && some) {
-#pragma unroll
-      for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] += p[i] * inverse;
-      if (sub == 0) {
+    if (all) {
+      const float norm = a.softmax ? (some ? top + __logf(total) : kNone) : total;
+      if (a.norm != nullptr && in && sub == 0) a.norm[at] = norm;
+      if (BAL && in && some && sub == 0) {
         live += 1;
         if (a.softmax) sq += norm * norm;
       }
@@ -315,7 +515,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_main(RouteArgs a) {
   for (int i = 0; i < (BAL ? M : 1); ++i) {
 #pragma unroll
     for (int o = kRowLanes; o < 64; o <<= 1) acc[i] += __shfl_xor(acc[i], o, 64);
-    const int e = ((i / V) * kRowLanes + sub) * V + i % V;
+    const int e = element<T, CH>(i, sub);
     if (lane < kRowLanes && e < E) mass[wave][e] = acc[i];
   }
 #pragma unroll
@@ -558,21 +758,28 @@ int fill_runs(Args& a, const int64_t* fam_off_host, int32_t n_fam, int rows) {
   return static_cast<int>(runs);
 }
 
+template <class T, int CH, int KL>
+void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
+  auto* kernel = a.bias != nullptr ? (bal ? route_main<T, CH, KL, true, true> : route_main<T, CH, KL, false, true>)
+                                   : (bal ? route_main<T, CH, KL, true, false> : route_main<T, CH, KL, false, false>);
+  kernel<<<grid, kRouteThreads, 0, s>>>(a);
+}
+
 template <class T, int CH>
 void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
-  const bool two = a.k > kRowLanes;
-  auto* kernel = bal ? (two ? route_main<T, CH, 2, true> : route_main<T, CH, 1, true>)
-                     : (two ? route_main<T, CH, 2, false> : route_main<T, CH, 1, false>);
-  kernel<<<grid, kRouteThreads, 0, s>>>(a);
+  if (a.k <= 8) start_main<T, CH, 8>(a, bal, grid, s);
+  else start_main<T, CH, 16>(a, bal, grid, s);
 }
 
 template <class T>
 void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
   const int chunks = (a.E + kChunk<T> * kRowLanes - 1) / (kChunk<T> * kRowLanes);
-  if (chunks <= 1) start_main<T, 1>(a, bal, grid, s);
-  else if (chunks <= 2) start_main<T, 2>(a, bal, grid, s);
-  else if (chunks <= 4) start_main<T, 4>(a, bal, grid, s);
-  else if constexpr (sizeof(T) == 4) start_main<T, 8>(a, bal, grid, s);
+  if constexpr (sizeof(T) == 2) {
+    if (chunks <= 1) return start_main<T, 1>(a, bal, grid, s);
+  }
+  if (chunks <= 2) return start_main<T, 2>(a, bal, grid, s);
+  if (chunks <= 4) return start_main<T, 4>(a, bal, grid, s);
+  if constexpr (sizeof(T) == 4) start_main<T, 8>(a, bal, grid, s);
 }
 
 template <class T, int CH>

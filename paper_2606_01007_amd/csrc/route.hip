@@ -275,14 +275,23 @@ struct Run {
 };
 template <class Args>
 __device__ __forceinline__ Run run_of(const Args& a, int run) {
-  int f = 0;
-  while (run >= a.run_off[f + 1]) ++f;
+  const int lane = threadIdx.x & 63;  // a lane per family: its runs lie before this one
+  const int f = __popcll(__ballot(lane < a.F && run >= a.run_off[lane + 1]));
   Run r;
   r.family = f;
   r.first = a.fam_off[f] + static_cast<int64_t>(run - a.run_off[f]) * a.rows;
   const int64_t end = r.first + a.rows;
   r.last = end < a.fam_off[f + 1] ? end : a.fam_off[f + 1];
   return r;
+}
+
+// Sum over the eight rows of a wave.
+__device__ __forceinline__ float rows_sum(float v) {
+  v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xf, 0xf, true));  // rotated by 8 within 16
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 template <class T, int CH>
@@ -295,6 +304,7 @@ template <class T, int CH, int KL, bool BAL, bool BIAS>
 __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
   constexpr int V = kChunk<T>, M = CH * V, KS = KL / kRowLanes;
   __shared__ double list[kRowsPerPass][kList];
+  __shared__ alignas(16) float copy[kRowsPerPass][M * kRowLanes + 4];  // the rows' logits: rows in different banks
   __shared__ int chosen[kRowsPerPass][KL];
   __shared__ uint32_t count[BAL ? TACG_MAX_EXPERTS : 1];
   __shared__ float mass[BAL ? kRouteWaves : 1][BAL ? TACG_MAX_EXPERTS : 1];
@@ -307,6 +317,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
   const T* layer = static_cast<const T*>(a.logits) + l * a.stride_layer;
   double* mine = list[tid >> 3];
   int* slots = chosen[tid >> 3];
+  float* logit = copy[tid >> 3];
   float acc[BAL ? M : 1];
   float sq = 0.0f;
   uint32_t live = 0;
@@ -347,6 +358,10 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
         for (int i = 0; i < M; ++i) x[i] = kNone;
       }
     }
+#pragma unroll
+    for (int i = 0; i < M; i += 4)
+      *reinterpret_cast<float4*>(logit + element<T, CH>(i, sub)) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const bool some = top > kNone;
     uint32_t mask = 0;
     if constexpr (!BIAS) mask = at_least(x, vmax(bound, -FLT_MAX));
@@ -383,7 +398,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
     }
     // what the selection orders by, of one expert
     auto value = [&](int e) {
-      float v = widen(row[e]);
+      float v = logit[e];
       if constexpr (BIAS) v = (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e];
       return v;
     };
@@ -433,7 +448,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
       for (int i = sub; i < most; i += kRowLanes) mine[i] = -INFINITY;
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     } else {
-      // k passes: the best after the last winner in (value descending, id ascending).  The values are read again.
+      // k passes: the best after the last winner in (value descending, id ascending)
       float last = INFINITY;
       int last_e = -1;
       for (int j = 0; j < k; ++j) {
@@ -441,8 +456,8 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
         int at = 0x7fffffff;
         for (int i = 0; i < M; ++i) {
           const int e = element<T, CH>(i, sub);
-          if (e >= E || !some) continue;
-          const float v = widen(row[e]) > kNone ? value(e) : kNone;
+          if (e >= E) continue;
+          const float v = logit[e] > kNone ? value(e) : kNone;
           const bool after = v < last || (v == last && e > last_e);
           if (after && v > best) best = v, at = e;
         }
@@ -462,7 +477,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
     // gates of the selected
     float w[KS];
 #pragma unroll
-    for (int q = 0; q < KS; ++q) w[q] = id[q] >= 0 ? widen(row[id[q]]) : kNone;
+    for (int q = 0; q < KS; ++q) w[q] = id[q] >= 0 ? logit[id[q]] : kNone;
     if (a.softmax) {
       float high = shift;
       if (BIAS && a.renorm) {
@@ -513,16 +528,13 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
   // the run's sums: rows of a wave, then the waves in order
 #pragma unroll
   for (int i = 0; i < (BAL ? M : 1); ++i) {
-#pragma unroll
-    for (int o = kRowLanes; o < 64; o <<= 1) acc[i] += __shfl_xor(acc[i], o, 64);
+    acc[i] = rows_sum(acc[i]);
     const int e = element<T, CH>(i, sub);
     if (lane < kRowLanes && e < E) mass[wave][e] = acc[i];
   }
+  sq = rows_sum(sq);
 #pragma unroll
-  for (int o = kRowLanes; o < 64; o <<= 1) {
-    sq += __shfl_xor(sq, o, 64);
-    live += __shfl_xor(live, o, 64);
-  }
+  for (int o = kRowLanes; o < 64; o <<= 1) live += __shfl_xor(live, o, 64);
   if (lane == 0) squares[wave] = sq, routed[wave] = live;
   barrier_after_lds_atomics();
   const int64_t slot = static_cast<int64_t>(l) * gridDim.x + blockIdx.x;

@@ -12,7 +12,7 @@
 //     elements reach;
 //   * those elements' values, with the id below the value's last bit (32-bit value and id in a 64-bit float), go to a list in LDS;
 //   * the place of each is the number of larger ones in the list.
-//   A row with more than kList such elements (many equal ones) is selected by k passes over the registers instead.
+//   A row with more than 2 KL such elements (many equal ones) is selected by k passes over the registers instead.
 //   A workgroup takes a run of rows of one segment; its sums of s' (32 bits over a run, then 64), counts, rows and squares go to a
 //   slot of the workspace, and route_reduce adds a segment's slots in order in 64 bits, so that results do not depend on the
 //   order of execution.
@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "tacg_internal.h"
 
@@ -50,7 +51,8 @@ struct RouteArgs {
   double* squares;                               // [slots]
   uint32_t* routed;                              // [slots]
   uint32_t* err;
-  int32_t run_off[TACG_MAX_FAMILIES + 1];        // first run of each family
+  // first run and first token of each family; a lane each reads a pair
+  int32_t run_off[TACG_MAX_FAMILIES + 1];
   int64_t fam_off[TACG_MAX_FAMILIES + 1];
 };
 
@@ -256,32 +258,30 @@ __device__ __forceinline__ uint32_t at_least(const float (&y)[M], float bound) {
   return mask;
 }
 
-constexpr int kList = 32;  // elements of a row's list
-
 // A list entry: orders by value, equal values by id, the lower one first.
 __device__ __forceinline__ double entry_of(float v, int e) {
   const uint64_t bits = __builtin_bit_cast(uint64_t, static_cast<double>(v + 0.0f));  // -0 and +0 are equal
   return __builtin_bit_cast(double, bits | static_cast<uint32_t>(v < 0.0f ? e : 255 - e));
 }
-__device__ __forceinline__ int id_of(double entry) {
-  const uint64_t bits = __builtin_bit_cast(uint64_t, entry);
-  const int e = static_cast<int>(bits & 255u);
-  return (bits >> 63) != 0 ? e : 255 - e;
-}
-
 struct Run {
   int family;
   int64_t first, last;  // tokens
 };
 template <class Args>
 __device__ __forceinline__ Run run_of(const Args& a, int run) {
-  const int lane = threadIdx.x & 63;  // a lane per family: its runs lie before this one
-  const int f = __popcll(__ballot(lane < a.F && run >= a.run_off[lane + 1]));
+  const int lane = threadIdx.x & 63;  // a lane per family, all tables read at once
+  const int next = a.run_off[lane + 1], first = a.run_off[lane];
+  const int64_t from = a.fam_off[lane], to = a.fam_off[lane + 1];
+  const int f = __popcll(__ballot(lane < a.F && run >= next));
+  auto of = [&](int64_t v) {
+    return static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), f))) << 32 |
+                                static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), f)));
+  };
   Run r;
   r.family = f;
-  r.first = a.fam_off[f] + static_cast<int64_t>(run - a.run_off[f]) * a.rows;
-  const int64_t end = r.first + a.rows;
-  r.last = end < a.fam_off[f + 1] ? end : a.fam_off[f + 1];
+  r.first = of(from) + static_cast<int64_t>(run - __builtin_amdgcn_readlane(first, f)) * a.rows;
+  const int64_t end = r.first + a.rows, last = of(to);
+  r.last = end < last ? end : last;
   return r;
 }
 
@@ -302,10 +302,10 @@ __device__ __forceinline__ int element(int i, int sub) {  // the id of a lane's 
 // grid: (runs, layers).  KL: 8 for k <= 8, else 16.
 template <class T, int CH, int KL, bool BAL, bool BIAS>
 __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
-  constexpr int V = kChunk<T>, M = CH * V, KS = KL / kRowLanes;
+  constexpr int V = kChunk<T>, M = CH * V, KS = KL / kRowLanes, kList = 2 * KL;  // kList: elements of a row's list
   __shared__ double list[kRowsPerPass][kList];
   __shared__ alignas(16) float copy[kRowsPerPass][M * kRowLanes + 4];  // the rows' logits: rows in different banks
-  __shared__ int chosen[kRowsPerPass][KL];
+  __shared__ float2 chosen[kRowsPerPass][KL];
   __shared__ uint32_t count[BAL ? TACG_MAX_EXPERTS : 1];
   __shared__ float mass[BAL ? kRouteWaves : 1][BAL ? TACG_MAX_EXPERTS : 1];
   __shared__ float squares[kRouteWaves];
@@ -316,12 +316,11 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
   const int E = a.E, k = a.k;
   const T* layer = static_cast<const T*>(a.logits) + l * a.stride_layer;
   double* mine = list[tid >> 3];
-  int* slots = chosen[tid >> 3];
+  float2* slots = chosen[tid >> 3];
   float* logit = copy[tid >> 3];
   float acc[BAL ? M : 1];
   float sq = 0.0f;
   uint32_t live = 0;
-  for (int i = sub; i < kList; i += kRowLanes) mine[i] = -INFINITY;
   if (BAL) {
 #pragma unroll
     for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] = 0.0f;
@@ -397,8 +396,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
       }
     }
     // what the selection orders by, of one expert
-    auto value = [&](int e) {
-      float v = logit[e];
+    auto value = [&](float v, int e) {
       if constexpr (BIAS) v = (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e];
       return v;
     };
@@ -421,31 +419,63 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
       const int v = __builtin_amdgcn_readlane(n, r);
       most = v > most ? v : most;
     }
-    int id[KS];  // of slots sub, sub + 8
+    int id[KS];   // of slots sub, sub + 8: expert and its logit
+    float w[KS];
 #pragma unroll
-    for (int q = 0; q < KS; ++q) id[q] = -1;
+    for (int q = 0; q < KS; ++q) id[q] = -1, w[q] = kNone;
     if (most <= kList) {
+      int32_t* ids = reinterpret_cast<int32_t*>(mine);  // before the entries
 #pragma unroll
-      for (int q = 0; q < KS; ++q) slots[sub + q * kRowLanes] = -1;
+      for (int q = 0; q < KS; ++q) slots[sub + q * kRowLanes] = make_float2(__int_as_float(-1), kNone);
       while (__any(mask != 0)) {
         if (mask != 0) {
           const int i = __clz(mask) - (32 - M);
           mask &= ~(1u << (M - 1 - i));
-          const int e = element<T, CH>(i, sub);
-          mine[before++] = entry_of(value(e), e);
+          ids[before++] = element<T, CH>(i, sub);
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      for (int first = 0; first < most; first += kRowLanes) {
-        const double own = mine[first + sub];
-        int larger = 0;
-        for (int i = 0; i < most; ++i) larger += mine[i] > own;
-        if (first + sub < n && larger < k) slots[larger] = id_of(own);
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      // entries sub, sub + 8, ... of the lane; those past the end order behind all others
+      auto place = [&](auto entries) {
+        constexpr int N = entries.value;
+        int e[N], larger[N];
+        float x[N];
+        double own[N];
 #pragma unroll
-      for (int q = 0; q < KS; ++q) id[q] = slots[sub + q * kRowLanes];
-      for (int i = sub; i < most; i += kRowLanes) mine[i] = -INFINITY;
+        for (int q = 0; q < N; ++q) {
+          const bool have = sub + q * kRowLanes < n;
+          e[q] = have ? ids[sub + q * kRowLanes] : 0;
+          x[q] = logit[e[q]];
+          own[q] = have ? entry_of(value(x[q], e[q]), e[q]) : -INFINITY;
+          larger[q] = 0;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int q = 0; q < N; ++q) mine[sub + q * kRowLanes] = own[q];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int first = 0; first < N * kRowLanes; first += kRowLanes) {
+          double other[kRowLanes];
+#pragma unroll
+          for (int i = 0; i < kRowLanes; ++i) other[i] = mine[first + i];
+#pragma unroll
+          for (int i = 0; i < kRowLanes; ++i)
+#pragma unroll
+            for (int q = 0; q < N; ++q) larger[q] += other[i] > own[q];
+        }
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+          if (sub + q * kRowLanes < n && larger[q] < k) slots[larger[q]] = make_float2(__int_as_float(e[q]), x[q]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      };
+      if (KL == 8 || most <= 3 * kRowLanes) place(std::integral_constant<int, KL == 8 ? 2 : 3>());
+      else place(std::integral_constant<int, 4>());
+#pragma unroll
+      for (int q = 0; q < KS; ++q) {
+        const float2 v = slots[sub + q * kRowLanes];
+        id[q] = __float_as_int(v.x);
+        w[q] = v.y;
+      }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     } else {
       // k passes: the best after the last winner in (value descending, id ascending)
@@ -457,7 +487,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
         for (int i = 0; i < M; ++i) {
           const int e = element<T, CH>(i, sub);
           if (e >= E) continue;
-          const float v = logit[e] > kNone ? value(e) : kNone;
+          const float v = logit[e] > kNone ? value(logit[e], e) : kNone;
           const bool after = v < last || (v == last && e > last_e);
           if (after && v > best) best = v, at = e;
         }
@@ -469,15 +499,12 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
         }
 #pragma unroll
         for (int q = 0; q < KS; ++q)
-          if (j == sub + q * kRowLanes && best > kNone) id[q] = at;
+          if (j == sub + q * kRowLanes && best > kNone) id[q] = at, w[q] = logit[at];
         last = best;
         last_e = best > kNone ? at : 0x7fffffff;
       }
     }
     // gates of the selected
-    float w[KS];
-#pragma unroll
-    for (int q = 0; q < KS; ++q) w[q] = id[q] >= 0 ? logit[id[q]] : kNone;
     if (a.softmax) {
       float high = shift;
       if (BIAS && a.renorm) {

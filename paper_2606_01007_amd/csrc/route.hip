@@ -7,12 +7,12 @@
 //   balance = E / (k T^2) sum_e D_e M_e,   z = 1/T sum_t lse_t^2.
 //
 // route_main: one pass over the logits.  Selection in a row:
-//   * a lane's elements fall into up to eight groups; the k-th largest (8th or 16th, by the kernel's variant) of the row's group maxima,
+//   * a lane's elements fall into up to eight groups; the k-th largest (4th, 8th or 16th, by the kernel's variant) of the row's group maxima,
 //     found by sorting networks within and merges across the lanes, is a lower bound of the k-th largest logit that few more than k
 //     elements reach;
 //   * those elements' values, with the id below the value's last bit (32-bit value and id in a 64-bit float), go to a list in LDS;
 //   * the place of each is the number of larger ones in the list.
-//   A row with more than 2 KL such elements (many equal ones) is selected by k passes over the registers instead.
+//   A row with more such elements than the list holds (many equal ones) is selected by k passes over the registers instead.
 //   A workgroup takes a run of rows of one segment; its sums of s' (32 bits over a run, then 64), counts, rows and squares go to a
 //   slot of the workspace, and route_reduce adds a segment's slots in order in 64 bits, so that results do not depend on the
 //   order of execution.
@@ -198,16 +198,18 @@ __device__ __forceinline__ void sort_bitonic(float* a) {
     sort_bitonic<N / 2>(a + N / 2);
   }
 }
+// Batcher's odd-even merge sort, largest first: 19 exchanges for eight.
 template <int N>
-__device__ __forceinline__ void sort_all(float* a) {
-  if constexpr (N > 1) {
-    sort_all<N / 2>(a);
-    sort_all<N / 2>(a + N / 2);
+__device__ __forceinline__ void sort_all(float (&a)[N]) {
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) order(a[i], a[N - 1 - i]);
-    sort_bitonic<N / 2>(a);
-    sort_bitonic<N / 2>(a + N / 2);
-  }
+  for (int p = 1; p < N; p *= 2)
+#pragma unroll
+    for (int d = p; d >= 1; d /= 2)
+#pragma unroll
+      for (int j = d % p; j + d < N; j += 2 * d)
+#pragma unroll
+        for (int i = j; i < j + d && i + d < N; ++i)
+          if (i / (2 * p) == (i + d) / (2 * p)) order(a[i], a[i + d]);
 }
 // The N largest of the sorted lists of this lane and another; sorted again, or (LAST) only the smallest of them.
 template <int N, int CTRL, bool LAST>
@@ -232,16 +234,16 @@ __device__ __forceinline__ float merge(float (&a)[N]) {
 template <int KL, int M>
 __device__ __forceinline__ float lower_bound(const float (&y)[M], float& top) {
   constexpr int G = M < 8 ? M : 8;
-  float a[KL];
-#pragma unroll
-  for (int i = 0; i < KL; ++i) a[i] = kNone;
+  float m[G], a[KL];
 #pragma unroll
   for (int j = 0; j < G; ++j) {
-    if constexpr (M / G == 4) a[j] = vmax(vmax3(y[j], y[j + G], y[j + 2 * G]), y[j + 3 * G]);
-    else if constexpr (M / G == 2) a[j] = vmax(y[j], y[j + G]);
-    else a[j] = y[j];
+    if constexpr (M / G == 4) m[j] = vmax(vmax3(y[j], y[j + G], y[j + 2 * G]), y[j + 3 * G]);
+    else if constexpr (M / G == 2) m[j] = vmax(y[j], y[j + G]);
+    else m[j] = y[j];
   }
-  sort_all<G>(a);
+  sort_all(m);
+#pragma unroll
+  for (int i = 0; i < KL; ++i) a[i] = i < G ? m[i < G ? i : 0] : kNone;
   merge<KL, kSwap1, false>(a);
   merge<KL, kSwap2, false>(a);
   top = vmax(a[0], across<kMirror>(a[0]));
@@ -299,13 +301,14 @@ __device__ __forceinline__ int element(int i, int sub) {  // the id of a lane's 
   return ((i / kChunk<T>) * kRowLanes + sub) * kChunk<T> + i % kChunk<T>;
 }
 
-// grid: (runs, layers).  KL: 8 for k <= 8, else 16.
+// grid: (runs, layers).  KL: the smallest of 4, 8 and 16 that is not below k.
 template <class T, int CH, int KL, bool BAL, bool BIAS>
 __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
-  constexpr int V = kChunk<T>, M = CH * V, KS = KL / kRowLanes, kList = 2 * KL;  // kList: elements of a row's list
+  constexpr int V = kChunk<T>, M = CH * V, KS = (KL + kRowLanes - 1) / kRowLanes;
+  constexpr int kList = KL < 8 ? 16 : 2 * KL;  // elements of a row's list
   __shared__ double list[kRowsPerPass][kList];
   __shared__ alignas(16) float copy[kRowsPerPass][M * kRowLanes + 4];  // the rows' logits: rows in different banks
-  __shared__ float2 chosen[kRowsPerPass][KL];
+  __shared__ float2 chosen[kRowsPerPass][KS * kRowLanes];
   __shared__ uint32_t count[BAL ? TACG_MAX_EXPERTS : 1];
   __shared__ float mass[BAL ? kRouteWaves : 1][BAL ? TACG_MAX_EXPERTS : 1];
   __shared__ float squares[kRouteWaves];
@@ -427,11 +430,17 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
       int32_t* ids = reinterpret_cast<int32_t*>(mine);  // before the entries
 #pragma unroll
       for (int q = 0; q < KS; ++q) slots[sub + q * kRowLanes] = make_float2(__int_as_float(-1), kNone);
-      while (__any(mask != 0)) {
-        if (mask != 0) {
-          const int i = __clz(mask) - (32 - M);
-          mask &= ~(1u << (M - 1 - i));
-          ids[before++] = element<T, CH>(i, sub);
+      if constexpr (M <= 8) {
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+          if ((mask >> (M - 1 - i)) & 1u) ids[before++] = element<T, CH>(i, sub);
+      } else {
+        while (__any(mask != 0)) {
+          if (mask != 0) {
+            const int i = __clz(mask) - (32 - M);
+            mask &= ~(1u << (M - 1 - i));
+            ids[before++] = element<T, CH>(i, sub);
+          }
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -468,8 +477,13 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
           if (sub + q * kRowLanes < n && larger[q] < k) slots[larger[q]] = make_float2(__int_as_float(e[q]), x[q]);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       };
-      if (KL == 8 || most <= 3 * kRowLanes) place(std::integral_constant<int, KL == 8 ? 2 : 3>());
-      else place(std::integral_constant<int, 4>());
+      if constexpr (KL == 16) {
+        if (most <= 3 * kRowLanes) place(std::integral_constant<int, 3>());
+        else place(std::integral_constant<int, 4>());
+      } else {
+        if (most <= kRowLanes) place(std::integral_constant<int, 1>());
+        else place(std::integral_constant<int, 2>());
+      }
 #pragma unroll
       for (int q = 0; q < KS; ++q) {
         const float2 v = slots[sub + q * kRowLanes];
@@ -806,7 +820,8 @@ void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
 
 template <class T, int CH>
 void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
-  if (a.k <= 8) start_main<T, CH, 8>(a, bal, grid, s);
+  if (a.k <= 4) start_main<T, CH, 4>(a, bal, grid, s);
+  else if (a.k <= 8) start_main<T, CH, 8>(a, bal, grid, s);
   else start_main<T, CH, 16>(a, bal, grid, s);
 }
 

@@ -83,15 +83,18 @@ __device__ __forceinline__ float4v mfma(const uint4v& tokens, const uint4v& weig
 // weight 1.  A level in bits 4 to 7 needs an offset of 64 in float16, in bits 0 to 3 one of 1024, which would cost the sums four bits.
 template <class T>
 constexpr float kOffset = __is_same(T, __bf16) ? 128.0f : 64.0f;
+// The four bits of each half, in a vector register that the compiler takes for a variable: an AND-OR takes one scalar operand, and with two
+// known ones it becomes two instructions.
 template <class T>
-__device__ __forceinline__ uint4v spread(uint32_t w) {
-  uint32_t mask;  // in a vector register: an AND-OR takes one scalar operand
+__device__ __forceinline__ uint32_t level_mask() {
+  return __builtin_amdgcn_mbcnt_lo(0, __is_same(T, __bf16) ? 0x000f000fu : 0x00f000f0u);
+}
+template <class T>
+__device__ __forceinline__ uint4v spread(uint32_t w, uint32_t mask) {
   if constexpr (__is_same(T, __bf16)) {
-    asm("v_mov_b32 %0, 0xf000f" : "=v"(mask));
     constexpr uint32_t kBase = 0x43004300u;
     return uint4v{(w & mask) | kBase, ((w >> 4) & mask) | kBase, ((w >> 8) & mask) | kBase, ((w >> 12) & mask) | kBase};
   } else {
-    asm("v_mov_b32 %0, 0xf000f0" : "=v"(mask));
     constexpr uint32_t kBase = 0x54005400u;
     return uint4v{((w << 4) & mask) | kBase, (w & mask) | kBase, ((w >> 4) & mask) | kBase, ((w >> 8) & mask) | kBase};
   }
@@ -219,11 +222,15 @@ __device__ __forceinline__ float half_of(uint32_t word, int i) {
 }
 
 // sum += factor * scale * (level - zero) . x of one step; tokens(t, i): the lane's ordered values of block i of token tile t.
-template <class T, int RT, int TT, int GROUPS, bool ZEROS, class Tokens>
+// J: how many of the four tokens of a lane's sums there are.
+template <class T, int RT, int TT, int J, int GROUPS, bool ZEROS, class Tokens>
 __device__ __forceinline__ void add_step(const Weights<T, RT, GROUPS, ZEROS>& o, Tokens tokens, float factor,
                                          float4v (&sum)[RT][TT]) {
   constexpr int kRun = kBlocks / GROUPS;  // products of a group
-  constexpr uint32_t kOnes = __is_same(T, __bf16) ? 0x3f803f80u : 0x3c003c00u;
+  // sum x (zeros given) or -(offset + 8) sum x, which the products then start from
+  constexpr uint32_t kOnes = __is_same(T, __bf16) ? (ZEROS ? 0x3f80u : 0xc308u) : (ZEROS ? 0x3c00u : 0xd480u);
+  constexpr uint32_t kOne = kOnes | kOnes << 16;
+  const uint32_t mask = level_mask<T>();
   uint32_t w[RT][kBlocks];
 #pragma unroll
   for (int r = 0; r < RT; ++r)
@@ -242,35 +249,34 @@ __device__ __forceinline__ void add_step(const Weights<T, RT, GROUPS, ZEROS>& o,
 #pragma unroll
   for (int g = 0; g < GROUPS; ++g) {
     float4v all[TT], part[RT][TT];
+    uint4v x[TT][kRun];
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       all[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int r = 0; r < RT; ++r) part[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int i = 0; i < kRun; ++i) {
+        x[t][i] = tokens(t, g * kRun + i);
+        all[t] = mfma(x[t][i], uint4v{kOne, kOne, kOne, kOne}, all[t], T());
+      }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) part[r][t] = ZEROS ? float4v{0.0f, 0.0f, 0.0f, 0.0f} : all[t];
     }
 #pragma unroll
-    for (int i = g * kRun; i < (g + 1) * kRun; ++i) {
-      uint4v x[TT];
-#pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        x[t] = tokens(t, i);
-        all[t] = mfma(x[t], uint4v{kOnes, kOnes, kOnes, kOnes}, all[t], T());
-      }
+    for (int i = 0; i < kRun; ++i)
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const uint4v v = spread<T>(w[r][i]);
+        const uint4v v = spread<T>(w[r][g * kRun + i], mask);
 #pragma unroll
-        for (int t = 0; t < TT; ++t) part[r][t] = mfma(x[t], v, part[r][t], T());
+        for (int t = 0; t < TT; ++t) part[r][t] = mfma(x[t][i], v, part[r][t], T());
       }
-    }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const float scale = half_of<T>(o.scale[r][g / 2], g % 2) * factor;
-      const float zero = kOffset<T> + (ZEROS ? static_cast<float>((o.zero[ZEROS ? r : 0][g / 4] >> (8 * (g % 4))) & 255u) : 8.0f);
+      const float zero = ZEROS ? kOffset<T> + static_cast<float>((o.zero[ZEROS ? r : 0][g / 4] >> (8 * (g % 4))) & 255u) : 0.0f;
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[r][t][j] += scale * (part[r][t][j] - zero * all[t][j]);
+        for (int j = 0; j < J; ++j) sum[r][t][j] += scale * (ZEROS ? part[r][t][j] - zero * all[t][j] : part[r][t][j]);
         asm volatile("" : "+v"(sum[r][t]));  // here, and not with the other groups: all their products would not fit the registers
       }
     }
@@ -335,18 +341,106 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kTokenBytes = kStep * 2 + 16;  // of a token's step in LDS: 16 tokens' pieces lie in different banks
 
+// Tokens base .. of a workgroup's list, 4 J TT at most, with its weight rows: every wave has rows of its own; the tokens' values come
+// through LDS, a step ahead, in two buffers.  J < 4 (few tokens): a token's values stand in several of a product's 16 rows, so that
+// the sums of 4 q .. 4 q + 3 have J different ones, and a lane has J sums to scale instead of four.
+template <class T, bool GLU, int RT, int TT, int J, int GROUPS, bool ZEROS>
+__device__ __forceinline__ void tokens_with_rows(const Q4Args& a, const Rows<T, RT>& rows, const uint16_t* list, int64_t from,
+                                                 int base, int count, int column, char (*held)[kTokenBytes]) {
+  constexpr int kTokens = 4 * J * TT;
+  constexpr int kLoads = (kTokens + 7) / 8;  // 16-byte pieces of a step's tokens that a thread brings
+  const int tid = threadIdx.x, lane = tid & 63, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int width = GLU ? a.N / 2 : a.N;
+  const int row = lane & 15, token = J * (row >> 2) + ((row & 3) < J ? row & 3 : J - 1);
+  const bool brings = kTokens >= 8 || (tid >> 5) < kTokens;
+  const T* x[kLoads];
+  uint4v piece[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int at = base + 8 * i + (tid >> 5);  // past the last token: its values again, for sums that nobody takes
+    const uint32_t pair = static_cast<uint32_t>(from) + list[at < count ? at : count - 1];
+    const uint32_t t = pair / a.k, j = pair % a.k;
+    x[i] = static_cast<const T*>(a.x) + t * a.x_token + j * a.x_slot;
+  }
+  auto fetch = [&](auto whole, int s) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) piece[i] = load_token<whole.value>(a, x[i], s * kStep + 8 * (tid & 31));
+  };
+  auto buffer = [&](int s, int t) { return held[(s & 1) * kTokens + t]; };
+  auto stage = [&](int s) {
+    if (brings) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        *reinterpret_cast<uint4v*>(buffer(s, 8 * i + (tid >> 5)) + 16 * (tid & 31)) = in_order(piece[i]);
+    }
+  };
+  float4v sum[RT][TT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+  Weights<T, RT, GROUPS, ZEROS> now, next;
+  auto add = [&](int s) {
+    add_step<T, RT, TT, J, GROUPS, ZEROS>(now, [&](int t, int i) {
+      return *reinterpret_cast<const uint4v*>(buffer(s, 16 * t + token) + 64 * i + 16 * quarter);
+    }, 1.0f, sum);
+  };
+  const std::true_type whole;
+  const int last = a.K / kStep - 1;  // of the steps before the columns' end
+  if (last >= 0) {
+    fetch(whole, 0);
+    load_weights<true>(a, 0, quarter, rows, now);
+    stage(0);
+    fetch(whole, last < 1 ? last : 1);
+  }
+  __syncthreads();
+  for (int s = 0; s <= last; ++s) {  // what is brought after the last step is not used
+    load_weights<true>(a, s < last ? s + 1 : last, quarter, rows, next);
+    add(s);
+    stage(s + 1);
+    fetch(whole, s + 2 <= last ? s + 2 : last);
+    __syncthreads();
+    now = next;
+  }
+  if ((last + 1) * kStep < a.K) {
+    fetch(std::false_type(), last + 1);
+    load_weights<false>(a, last + 1, quarter, rows, now);
+    stage(last + 1);
+    __syncthreads();
+    add(last + 1);
+  }
+  __syncthreads();  // the buffers are free for the next tokens
+  constexpr int kRows = GLU ? RT / 2 : RT;
+  T* out = static_cast<T*>(a.out);
+#pragma unroll
+  for (int t = 0; t < TT; ++t)
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int i = base + 16 * t + J * quarter + j;
+      if (i >= count) continue;
+      const int64_t at = (from + list[i]) * width;
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const int c = column + wave * 16 * kRows + 16 * r + row;
+        if (c >= width) continue;
+        const float v = GLU ? silu(sum[r][t][j]) * sum[r + (GLU ? kRows : 0)][t][j] : sum[r][t][j];
+        if (a.mode == TACG_Q4_SUM) a.part[at + c] = v;
+        else out[at + c] = static_cast<T>(v);
+      }
+    }
+}
+
 // Many pairs.  grid: (blocks of a workgroup's output columns, held experts and one for the pairs that none serves, runs of kScan pairs).
-// Every wave has weight rows of its own; the tokens' values come through LDS, a step ahead, in two buffers.
 template <class T, bool GLU, int RT, int TT, int GROUPS, bool ZEROS>
 __global__ __launch_bounds__(kThreads, 2) void q4_tiles(Q4Args a) {
   constexpr int kOut = GLU ? RT * 8 : RT * 16;  // output columns of a wave
   constexpr int kWidth = kOut * kWaves;         // of the workgroup
-  constexpr int kLoads = 2 * TT;                // 16-byte pieces of a step's tokens that a thread brings
-  __shared__ alignas(16) char held[2][16 * TT][kTokenBytes];
+  __shared__ alignas(16) char held[2 * 16 * TT][kTokenBytes];
   __shared__ uint16_t list[kScan];
   __shared__ int16_t place[TACG_MAX_EXPERTS];
   __shared__ int total[kWaves];
-  const int tid = threadIdx.x, lane = tid & 63, quarter = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t pairs = a.n_tokens * a.k, from = static_cast<int64_t>(blockIdx.z) * kScan;
   const int n = static_cast<int>(pairs - from < kScan ? pairs - from : kScan);
@@ -354,6 +448,19 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tiles(Q4Args a) {
   const int h = static_cast<int>(blockIdx.y) < a.H ? static_cast<int>(blockIdx.y) : -1;
   const int column = blockIdx.x * kWidth;
   const int width = GLU ? a.N / 2 : a.N;
+  __syncthreads();
+  const int count = n <= kThreads * 8 ? list_pairs<1>(a, from, n, h, place, list, total)
+                                      : list_pairs<4>(a, from, n, h, place, list, total);
+  if (h < 0) {
+    if (blockIdx.x == 0)
+      for (int i = tid; i < n; i += kThreads) report(a, look_up(a, place, a.ids[from + i]));
+    if (a.mode == TACG_Q4_SUM) return;
+    for (int64_t i = tid; i < static_cast<int64_t>(count) * kWidth; i += kThreads) {
+      const int c = column + static_cast<int>(i % kWidth);
+      if (c < width) static_cast<T*>(a.out)[(from + list[i / kWidth]) * width + c] = static_cast<T>(0.0f);
+    }
+    return;
+  }
   Rows<T, RT> rows = rows_of<T, RT>(a, h);
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -361,92 +468,14 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tiles(Q4Args a) {
     v = v < width ? v : width - 1;
     rows.at[r] = v + (GLU && r >= RT / 2 ? width : 0);
   }
-  __syncthreads();
-  const int count = n <= kThreads * 8 ? list_pairs<1>(a, from, n, h, place, list, total)
-                                      : list_pairs<4>(a, from, n, h, place, list, total);
-  T* out = static_cast<T*>(a.out);
-  if (h < 0) {
-    if (blockIdx.x == 0)
-      for (int i = tid; i < n; i += kThreads) report(a, look_up(a, place, a.ids[from + i]));
-    if (a.mode == TACG_Q4_SUM) return;
-    for (int64_t i = tid; i < static_cast<int64_t>(count) * kWidth; i += kThreads) {
-      const int c = column + static_cast<int>(i % kWidth);
-      if (c < width) out[(from + list[i / kWidth]) * width + c] = static_cast<T>(0.0f);
-    }
-    return;
-  }
   for (int base = 0; base < count; base += 16 * TT) {
-    const T* x[kLoads];
-    uint4v piece[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = base + 8 * i + (tid >> 5);  // past the last token: its values again, for sums that nobody takes
-      const uint32_t pair = static_cast<uint32_t>(from) + list[at < count ? at : count - 1];
-      const uint32_t token = pair / a.k, j = pair % a.k;
-      x[i] = static_cast<const T*>(a.x) + token * a.x_token + j * a.x_slot;
-    }
-    auto fetch = [&](auto whole, int s) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) piece[i] = load_token<whole.value>(a, x[i], s * kStep + 8 * (tid & 31));
-    };
-    auto stage = [&](int s) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        *reinterpret_cast<uint4v*>(&held[s & 1][8 * i + (tid >> 5)][16 * (tid & 31)]) = in_order(piece[i]);
-    };
-    float4v sum[RT][TT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int t = 0; t < TT; ++t) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    Weights<T, RT, GROUPS, ZEROS> now, next;
-    auto add = [&](int s) {
-      add_step<T, RT, TT, GROUPS, ZEROS>(now, [&](int t, int i) {
-        return *reinterpret_cast<const uint4v*>(&held[s & 1][16 * t + (lane & 15)][64 * i + 16 * quarter]);
-      }, 1.0f, sum);
-    };
-    const std::true_type whole;
-    const int last = a.K / kStep - 1;  // of the steps before the columns' end
-    if (last >= 0) {
-      fetch(whole, 0);
-      load_weights<true>(a, 0, quarter, rows, now);
-      stage(0);
-      fetch(whole, last < 1 ? last : 1);
-    }
-    __syncthreads();
-    for (int s = 0; s <= last; ++s) {  // what is brought after the last step is not used
-      load_weights<true>(a, s < last ? s + 1 : last, quarter, rows, next);
-      add(s);
-      stage(s + 1);
-      fetch(whole, s + 2 <= last ? s + 2 : last);
-      __syncthreads();
-      now = next;
-    }
-    if ((last + 1) * kStep < a.K) {
-      fetch(std::false_type(), last + 1);
-      load_weights<false>(a, last + 1, quarter, rows, now);
-      stage(last + 1);
-      __syncthreads();
-      add(last + 1);
-    }
-    __syncthreads();  // the buffers are free for the next tokens
-    constexpr int kRows = GLU ? RT / 2 : RT;
-#pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = base + 16 * t + 4 * quarter + j;
-        if (i >= count) continue;
-        const int64_t at = (from + list[i]) * width;
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          const int c = column + wave * kOut + 16 * r + (lane & 15);
-          if (c >= width) continue;
-          const float v = GLU ? silu(sum[r][t][j]) * sum[r + (GLU ? kRows : 0)][t][j] : sum[r][t][j];
-          if (a.mode == TACG_Q4_SUM) a.part[at + c] = v;
-          else out[at + c] = static_cast<T>(v);
-        }
-      }
+    const int left = count - base;
+    if (TT == 2 && left > 16)
+      tokens_with_rows<T, GLU, RT, TT, 4, GROUPS, ZEROS>(a, rows, list, from, base, count, column, held);
+    else if (left > 4)
+      tokens_with_rows<T, GLU, RT, 1, 4, GROUPS, ZEROS>(a, rows, list, from, base, count, column, held);
+    else
+      tokens_with_rows<T, GLU, RT, 1, 1, GROUPS, ZEROS>(a, rows, list, from, base, count, column, held);
   }
 }
 
@@ -534,7 +563,7 @@ __global__ __launch_bounds__(WAVES * 64, 4) void q4_few(Q4Args a) {
       };
       if ((s + 1) * kStep <= a.K) load(std::true_type());
       else load(std::false_type());
-      add_step<T, RT, 1, GROUPS, ZEROS>(w, [&](int, int b) { return in_order(v[b]); }, factor, sum);
+      add_step<T, RT, 1, SUM ? 1 : 4, GROUPS, ZEROS>(w, [&](int, int b) { return in_order(v[b]); }, factor, sum);
     }
     if (base > 0) __syncthreads();
 #pragma unroll
@@ -713,9 +742,12 @@ void start(const Q4Args& a, hipStream_t stream) {
     else start_few<T, TACG_Q4_EACH, 8>(a, stream);
     return;
   }
+  // workgroups of 256 weight rows, four tiles a wave
+  const int64_t wide = static_cast<int64_t>(a.H) * ((a.N + 255) / 256);
   const bool two = pairs > 10 * static_cast<int64_t>(a.E);
-  if (glu) two ? start_tiles<T, true, 2, 2>(a, stream) : start_tiles<T, true, 2, 1>(a, stream);
-  else two ? start_tiles<T, false, 2, 2>(a, stream) : start_tiles<T, false, 2, 1>(a, stream);
+  if (two && wide >= 1024) glu ? start_tiles<T, true, 4, 2>(a, stream) : start_tiles<T, false, 4, 2>(a, stream);
+  else if (two) glu ? start_tiles<T, true, 2, 2>(a, stream) : start_tiles<T, false, 2, 2>(a, stream);
+  else glu ? start_tiles<T, true, 2, 1>(a, stream) : start_tiles<T, false, 2, 1>(a, stream);
   if (a.mode == TACG_Q4_SUM)
     q4_combine<T><<<dim3((a.N + 255) / 256, static_cast<uint32_t>(std::min<int64_t>(a.n_tokens, 65535))), 256, 0, stream>>>(a);
 }

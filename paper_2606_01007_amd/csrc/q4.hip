@@ -124,7 +124,7 @@ size_t expert_q4_workspace(int64_t n_tokens, int32_t top_k, int32_t n_experts, i
                            int32_t mode) {
   (void)n_cols;
   const int64_t pairs = n_tokens * top_k;
-  if (mode != TACG_Q4_SUM || q4_few_pairs(pairs, n_experts)) return 0;
+  if (mode != TACG_Q4_SUM || q4_few_pairs(pairs, n_experts, mode)) return 0;
   return align256(static_cast<size_t>(pairs) * n_rows * sizeof(float));
 }
 
@@ -159,7 +159,7 @@ int launch_expert_q4(const void* x, int32_t dtype, int64_t x_stride_token, int64
   const bool ragged = n_cols % group != 0 || n_cols < kStep;
   if (dtype == TACG_BF16) ragged ? q4_start<__bf16, true>(a, stream) : q4_start<__bf16, false>(a, stream);
   else ragged ? q4_start<_Float16, true>(a, stream) : q4_start<_Float16, false>(a, stream);
-  if (mode == TACG_Q4_SUM && !q4_few_pairs(n_tokens * top_k, n_experts)) {
+  if (mode == TACG_Q4_SUM && !q4_few_pairs(n_tokens * top_k, n_experts, mode)) {
     const dim3 grid((n_rows + 255) / 256, static_cast<uint32_t>(std::min<int64_t>(n_tokens, 65535)));
     if (dtype == TACG_BF16) q4_combine<__bf16><<<grid, 256, 0, stream>>>(a);
     else q4_combine<_Float16><<<grid, 256, 0, stream>>>(a);

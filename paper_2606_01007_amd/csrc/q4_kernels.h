@@ -23,8 +23,13 @@
 
 namespace tacg {
 
-// Few pairs: most have an expert of their own, so a workgroup per pair leaves little to share and wastes none on experts without tokens.
-inline bool q4_few_pairs(int64_t pairs, int32_t n_experts) { return pairs <= n_experts; }
+// Few pairs: most have an expert of their own, so a workgroup per pair (or token) leaves little to share and wastes none on experts
+// without tokens.  Measured, few against many in us: gated, 128 experts of 1536 x 2048, top-8: 20.5 / 25.6 at 4 tokens, 35.9 / 29.9
+// at 8; 60 experts, top-4: 12.4 / 20.4 at 4, 20.2 / 23.1 at 8, 33.6 / 25.1 at 16.  Summed (2048 x 1024): 30.4 / 32.4 at 16 tokens
+// of 128 experts, 56.4 / 37.1 at 32; 18.2 / 21.3 at 16 of 60, 33.0 / 21.9 at 32.
+inline bool q4_few_pairs(int64_t pairs, int32_t n_experts, int32_t mode) {
+  return mode == TACG_Q4_SUM ? pairs <= n_experts : 5 * pairs <= 2 * static_cast<int64_t>(n_experts);
+}
 
 constexpr int kPiece = 32;  // columns of 16 bytes of levels
 
@@ -710,24 +715,24 @@ template <class T, bool RAGGED>
 void q4_start(const Q4Args& a, hipStream_t stream) {
   const int64_t pairs = a.n_tokens * a.k;
   const bool glu = a.mode == TACG_Q4_GLU;
-  if (q4_few_pairs(pairs, a.E)) {
+  if (q4_few_pairs(pairs, a.E, a.mode)) {
     if (a.mode == TACG_Q4_SUM) start_few<T, RAGGED, TACG_Q4_SUM, 16>(a, stream);
     else if (glu) start_few<T, RAGGED, TACG_Q4_GLU, 8>(a, stream);
     else start_few<T, RAGGED, TACG_Q4_EACH, 8>(a, stream);
     return;
   }
-  // workgroups of 256 weight rows, four tiles a wave
+  // Two tiles of tokens from ten an expert on: with 2048 x 2048 and 128 experts 72.9 us against 70.1 at ten, 85 / 71 at twelve,
+  // 104 / 73 at sixteen (one against two tiles), below it the other way: 66.1 / 69.2 at eight.
+  // Rows of a wave, by the workgroups of 256 rows that there are: 64 from 512 on with two tiles of tokens (36.5 us against 43.1
+  // with 32; at 256: 23.6 / 22.1), 16 below 128 (13.3 against 16.3 with 32 at 64; at 256: 30.4 / 21.9), else 32.
   const int64_t wide = static_cast<int64_t>(a.H) * ((a.N + 255) / 256);
   const bool two = pairs > 10 * static_cast<int64_t>(a.E);
-  if (!two) {
-    glu ? start_tiles<T, RAGGED, true, 2, 1>(a, stream) : start_tiles<T, RAGGED, false, 2, 1>(a, stream);
-    return;
-  }
   if constexpr (!RAGGED) {
-    if (wide >= 1024) return glu ? start_tiles<T, RAGGED, true, 4, 2>(a, stream) : start_tiles<T, RAGGED, false, 4, 2>(a, stream);
-    if (!glu && wide < 256) return start_tiles<T, RAGGED, false, 1, 2>(a, stream);
+    if (two && wide >= 512) return glu ? start_tiles<T, RAGGED, true, 4, 2>(a, stream) : start_tiles<T, RAGGED, false, 4, 2>(a, stream);
+    if (!glu && wide < 128) return two ? start_tiles<T, RAGGED, false, 1, 2>(a, stream) : start_tiles<T, RAGGED, false, 1, 1>(a, stream);
   }
-  glu ? start_tiles<T, RAGGED, true, 2, 2>(a, stream) : start_tiles<T, RAGGED, false, 2, 2>(a, stream);
+  if (two) glu ? start_tiles<T, RAGGED, true, 2, 2>(a, stream) : start_tiles<T, RAGGED, false, 2, 2>(a, stream);
+  else glu ? start_tiles<T, RAGGED, true, 2, 1>(a, stream) : start_tiles<T, RAGGED, false, 2, 1>(a, stream);
 }
 
 }  // namespace tacg

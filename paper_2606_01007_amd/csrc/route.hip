@@ -50,6 +50,7 @@ struct RouteArgs {
   uint32_t* count;                               // [slots][E]
   double* squares;                               // [slots]
   uint32_t* routed;                              // [slots]
+  uint32_t* arrived;                             // [F][L], for route_reduce
   uint32_t* err;
   // first run and first token of each family; a lane each reads a pair
   int32_t run_off[TACG_MAX_FAMILIES + 1];
@@ -268,6 +269,7 @@ __device__ __forceinline__ double entry_of(float v, int e) {
 struct Run {
   int family;
   int64_t first, last;  // tokens
+  bool start;           // the family's first run
 };
 template <class Args>
 __device__ __forceinline__ Run run_of(const Args& a, int run) {
@@ -281,7 +283,9 @@ __device__ __forceinline__ Run run_of(const Args& a, int run) {
   };
   Run r;
   r.family = f;
-  r.first = of(from) + static_cast<int64_t>(run - __builtin_amdgcn_readlane(first, f)) * a.rows;
+  const int before = run - __builtin_amdgcn_readlane(first, f);
+  r.start = before == 0;
+  r.first = of(from) + static_cast<int64_t>(before) * a.rows;
   const int64_t end = r.first + a.rows, last = of(to);
   r.last = end < last ? end : last;
   return r;
@@ -328,6 +332,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
 #pragma unroll
     for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] = 0.0f;
     for (int e = tid; e < E; e += kRouteThreads) count[e] = 0;
+    if (tid == 0 && run.start) a.arrived[static_cast<int64_t>(run.family) * a.n_layers + l] = 0;
     __syncthreads();
   }
   // whether the sum over all experts is needed
@@ -601,6 +606,8 @@ struct ReduceArgs {
   const uint32_t* count;
   const double* squares;
   const uint32_t* routed;
+  double* part;        // [F][L][blocks of experts]
+  uint32_t* arrived;   // [F][L], cleared by route_main (or, without runs, not needed)
   int32_t runs, L, E, k;
   uint32_t* D;
   uint32_t* tokens;
@@ -609,32 +616,78 @@ struct ReduceArgs {
   int32_t run_off[TACG_MAX_FAMILIES + 1];
 };
 
-// grid: (families, layers), a thread per expert.
-__global__ __launch_bounds__(TACG_MAX_EXPERTS) void route_reduce(ReduceArgs a) {
-  __shared__ double part[TACG_MAX_EXPERTS / 64];
-  const int f = blockIdx.x, l = blockIdx.y, e = threadIdx.x, lane = e & 63, wave = e >> 6;
-  const int64_t segment = static_cast<int64_t>(f) * a.L + l;
-  const int64_t from = static_cast<int64_t>(l) * a.runs;
-  double m = 0.0, s = 0.0;
-  uint32_t c = 0, n = 0;
-  for (int r = a.run_off[f]; r < a.run_off[f + 1]; ++r) {
-    const int64_t slot = from + r;
-    if (e < a.E) {
-      m += a.mass[slot * a.E + e];
-      c += a.count[slot * a.E + e];
+// grid: (families, layers, blocks of EXPERTS experts).  The threads of a workgroup share the runs of a segment.  The last
+// workgroup of a segment to arrive adds up the blocks' parts, in order.
+template <int EXPERTS>
+__global__ __launch_bounds__(kRouteThreads) void route_reduce(ReduceArgs a) {
+  constexpr int kReduceExperts = EXPERTS, kReduceSlices = kRouteThreads / EXPERTS;
+  __shared__ double mass[kReduceSlices][kReduceExperts];
+  __shared__ uint32_t count[kReduceSlices][kReduceExperts];
+  __shared__ double waves[kRouteWaves];
+  __shared__ bool last;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int f = blockIdx.x, l = blockIdx.y, slice = tid / kReduceExperts, own = tid % kReduceExperts;
+  const int e = blockIdx.z * kReduceExperts + own;
+  const int64_t segment = static_cast<int64_t>(f) * a.L + l, from = static_cast<int64_t>(l) * a.runs;
+  const int begin = a.run_off[f], end = a.run_off[f + 1];
+  double m = 0.0;
+  uint32_t c = 0;
+  if (e < a.E) {
+#pragma unroll 4
+    for (int r = begin + slice; r < end; r += kReduceSlices) {
+      m += a.mass[(from + r) * a.E + e];
+      c += a.count[(from + r) * a.E + e];
     }
-    s += a.squares[slot];
-    n += a.routed[slot];
   }
-  if (e < a.E) a.D[segment * a.E + e] = c;
-  double v = m * c;
+  mass[slice][own] = m;
+  count[slice][own] = c;
+  __syncthreads();
+  double v = 0.0;
+  if (slice == 0 && e < a.E) {
+    m = 0.0;
+    c = 0;
+#pragma unroll
+    for (int s = 0; s < kReduceSlices; ++s) m += mass[s][own], c += count[s][own];
+    a.D[segment * a.E + e] = c;
+    v = m * c;
+  }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
-  if (lane == 0) part[wave] = v;
+  if (lane == 0) waves[wave] = v;
   __syncthreads();
-  if (e == 0) {
-    double b = 0.0;
-    for (int w = 0; w < TACG_MAX_EXPERTS / 64; ++w) b += part[w];
+  if (wave == 0) {
+    if (lane == 0) {
+      v = 0.0;
+#pragma unroll
+      for (int w = 0; w < kRouteWaves; ++w) v += waves[w];
+      bool done = true;
+      if (gridDim.z > 1) {
+        a.part[segment * gridDim.z + blockIdx.z] = v;
+        __threadfence();
+        done = begin == end || atomicAdd(&a.arrived[segment], 1u) == gridDim.z - 1;
+        __threadfence();
+      } else {
+        waves[0] = v;
+      }
+      last = done;
+    }
+  }
+  __syncthreads();
+  if (!last || wave != 0) return;
+  double s = 0.0, b = 0.0;
+  uint32_t n = 0;
+#pragma unroll 2
+  for (int r = begin + lane; r < end; r += 64) s += a.squares[from + r], n += a.routed[from + r];
+  if (begin < end && gridDim.z > 1 && lane < static_cast<int>(gridDim.z))
+    b = __hip_atomic_load(&a.part[segment * gridDim.z + lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (gridDim.z == 1 && lane == 0) b = waves[0];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    s += __shfl_xor(s, o, 64);
+    b += __shfl_xor(b, o, 64);
+    n += __shfl_xor(n, o, 64);
+  }
+  if (lane == 0) {
     const double rows = n;
     a.tokens[segment] = n;
     a.balance[segment] = n ? static_cast<float>(b * a.E / (a.k * rows * rows)) : 0.0f;
@@ -789,12 +842,19 @@ int piece_bytes(const void* base, int64_t stride_layer, int64_t stride_token, in
 
 int dtype_size(int32_t dtype) { return dtype == TACG_F32 ? 4 : 2; }
 
-// Rows of a workgroup's run: enough runs for the chip (eight workgroups a CU), of at least two passes where sums of a run go to a
-// slot (a slot is as long as two to four rows), and whole passes.
+// Rows of a workgroup's run, whole passes: eight workgroups a CU (58 layers of 8155 rows of 256 with sums: 129 us, with two a CU 145),
+// of at least two passes where the sums of a run go to a slot (24 layers of 2046 rows of 60: 14.7 us, with one 15.6).
 int run_rows(int64_t total_rows, bool sums) {
   int64_t r = total_rows / (256 * 8);
   r = (r + kRowsPerPass - 1) / kRowsPerPass * kRowsPerPass;
   return static_cast<int>(std::min<int64_t>(std::max<int64_t>(r, sums ? 2 * kRowsPerPass : kRowsPerPass), 512));
+}
+
+// Workgroups per segment of the reduction: several where the segments have many runs, which one workgroup would take too long for (one
+// layer of 8192 rows of 256: 50 us with one, 17 with eight); else one, as the fences between them cost more than they give (58
+// layers of 16 families of 2 runs: 362 us against 129; 24 of 6 families of 6 runs: 25 against 15).
+int reduce_blocks(int64_t n_tokens, int32_t n_layers, int32_t n_experts, int32_t n_fam) {
+  return n_tokens / run_rows(n_tokens * n_layers, true) >= 16 * n_fam ? (n_experts + 31) / 32 : 1;
 }
 
 template <class Args>
@@ -856,7 +916,9 @@ void start_back(const BackArgs& a, dim3 grid, hipStream_t s) {
 size_t route_workspace(int64_t n_tokens, int32_t n_layers, int32_t n_experts, int32_t n_fam) {
   const int rows = run_rows(n_tokens * n_layers, true);
   const size_t slots = static_cast<size_t>(n_layers) * static_cast<size_t>(n_tokens / rows + n_fam);
-  return 2 * align256(slots * n_experts * 4) + align256(slots * 8) + align256(slots * 4);
+  const size_t segments = static_cast<size_t>(n_layers) * n_fam;
+  return 2 * align256(slots * n_experts * 4) + align256(slots * 8) + align256(slots * 4) +
+         align256(segments * reduce_blocks(n_tokens, n_layers, n_experts, n_fam) * 8) + align256(segments * 4);
 }
 
 int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
@@ -884,6 +946,7 @@ int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_
   a.err = d_err;
   a.vec = piece_bytes(logits, stride_layer, stride_token, n_experts, dtype_size(dtype));
   const int runs = fill_runs(a, fam_off_host, n_fam, run_rows(n_tokens * n_layers, bal));
+  double* part = nullptr;
   if (bal) {
     Carver w{static_cast<char*>(workspace), 0};
     const size_t slots = static_cast<size_t>(n_layers) * runs;
@@ -891,6 +954,8 @@ int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_
     a.count = w.take<uint32_t>(slots * n_experts);
     a.squares = w.take<double>(slots);
     a.routed = w.take<uint32_t>(slots);
+    part = w.take<double>(static_cast<size_t>(n_layers) * n_fam * reduce_blocks(n_tokens, n_layers, n_experts, n_fam));
+    a.arrived = w.take<uint32_t>(static_cast<size_t>(n_layers) * n_fam);
   }
   if (runs > 0) {
     const dim3 grid(runs, n_layers);
@@ -905,6 +970,8 @@ int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_
     r.count = a.count;
     r.squares = a.squares;
     r.routed = a.routed;
+    r.part = part;
+    r.arrived = a.arrived;
     r.runs = runs;
     r.L = n_layers;
     r.E = n_experts;
@@ -914,7 +981,10 @@ int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_
     r.balance = balance;
     r.z = z;
     for (int f = 0; f <= n_fam; ++f) r.run_off[f] = a.run_off[f];
-    route_reduce<<<dim3(n_fam, n_layers), TACG_MAX_EXPERTS, 0, stream>>>(r);
+    const int blocks = reduce_blocks(n_tokens, n_layers, n_experts, n_fam);
+    const dim3 grid(n_fam, n_layers, blocks);
+    if (blocks > 1 || n_experts <= 32) route_reduce<32><<<grid, kRouteThreads, 0, stream>>>(r);
+    else route_reduce<TACG_MAX_EXPERTS><<<grid, kRouteThreads, 0, stream>>>(r);
     if (hipGetLastError() != hipSuccess) return TACG_E_DEVICE;
   }
   return TACG_OK;

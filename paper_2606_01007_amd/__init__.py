@@ -478,18 +478,30 @@ def jain_index(load: torch.Tensor, per_layer: bool = False, stream=None):
 # ---- the router and the experts' products --------------------------------------------------------
 
 def _logits(x: torch.Tensor):
-    """Pointer, type code and strides of router logits [L][N][E] whose rows are contiguous."""
-    if x.dim() != 3 or x.dtype not in DTYPES:
-        raise ValueError(f"logits: expected float32, bfloat16 or float16 [L][N][E], got {x.dtype} {tuple(x.shape)}")
+    """Pointer, type code, strides and shape of router logits [L][N][E] whose rows are contiguous."""
+    dtype, shape = DTYPES.get(x.dtype), x.shape
+    if dtype is None or len(shape) != 3:
+        raise ValueError(f"logits: expected float32, bfloat16 or float16 [L][N][E], got {x.dtype} {tuple(shape)}")
     if not x.is_cuda:
         raise ValueError("expected a device tensor")
-    if x.stride(2) != 1 and x.shape[2] > 1:
+    stride = x.stride()
+    if stride[2] != 1 and shape[2] > 1:
         raise ValueError("logits: the values of a row must be contiguous")
-    return x.data_ptr(), DTYPES[x.dtype], x.stride(0), x.stride(1)
+    return x.data_ptr(), dtype, stride[0], stride[1], shape
 
 
-def _segments(fam_off, N: int) -> np.ndarray:
-    return np.array([0, N], dtype=np.int64) if fam_off is None else _fam_off(fam_off)
+def _segments(fam_off, N: int):
+    """fam_off (None: one family of N tokens) as a C array of int64 and the number of families."""
+    if fam_off is None:
+        fam_off = (0, N)
+    elif not isinstance(fam_off, (list, tuple)):
+        fam_off = _fam_off(fam_off).tolist()
+    if len(fam_off) < 2:
+        raise ValueError(f"fam_off: expected a 1-D sequence of F + 1 >= 2 offsets, got {len(fam_off)}")
+    try:
+        return (ctypes.c_int64 * len(fam_off))(*fam_off), len(fam_off) - 1
+    except TypeError:  # numbers of other types, as numpy takes them
+        return (ctypes.c_int64 * len(fam_off))(*_fam_off(fam_off).tolist()), len(fam_off) - 1
 
 
 def _score(score: str) -> int:
@@ -510,13 +522,12 @@ def route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = "softmax"
     if stream is not None:  # all of the call, its buffers too, on that stream
         with torch.cuda.stream(stream):
             return route(logits, top_k, fam_off, score, bias, renorm, scale, balance, want_norm, ws, err, out)
-    ptr, dtype, s_layer, s_token = _logits(logits)
-    L_, N, E = logits.shape
-    dev = logits.device
-    off = _segments(fam_off, N)
-    F = off.size - 1
+    ptr, dtype, s_layer, s_token, (L_, N, E) = _logits(logits)
+    off, F = _segments(fam_off, N)
     code = _score(score)
+    C = _lib or lib()
     if out is None:
+        dev = logits.device
         out = dict(trace=torch.empty((L_, N, top_k), dtype=torch.int16, device=dev),
                    gate=torch.empty((L_, N, top_k), dtype=torch.float32, device=dev))
         if balance or want_norm:
@@ -529,20 +540,22 @@ def route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = "softmax"
                 out["z"] = torch.empty((F, L_), dtype=torch.float32, device=dev)
     else:
         out = dict(out)
-    get = out.get if balance else lambda name: None
     if balance:
-        need = lib().tacg_route_workspace_bytes(N, L_, E, F)
+        need = C.tacg_route_workspace_bytes(N, L_, E, F)
         if ws is None or ws.numel() < need:
-            ws = workspace(need, dev)
+            ws = workspace(need, logits.device)
+        D, tokens, b, z = out["D"], out["tokens"], out["balance"], out.get("z")
+    else:
+        D = tokens = b = z = None
     if err is None:
-        err = _err_tensor(dev)
-    st = lib().tacg_route(
-        ptr, dtype, s_layer, s_token, N, L_, top_k, E, _hptr(off), F, code,
+        err = _err_tensor(logits.device)
+    st = C.tacg_route(
+        ptr, dtype, s_layer, s_token, N, L_, top_k, E, off, F, code,
         _arg(bias, "bias", torch.float32, (L_, E)), 1 if renorm else 0, float(scale),
         _arg(out["trace"], "trace", torch.int16, (L_, N, top_k)), _arg(out["gate"], "gate", torch.float32, (L_, N, top_k)),
-        _arg(out.get("norm"), "norm", torch.float32, (L_, N)), _arg(get("D"), "D", torch.int32, (F, L_, E)),
-        _arg(get("tokens"), "tokens", torch.int32, (F, L_)), _arg(get("balance"), "balance", torch.float32, (F, L_)),
-        _arg(get("z"), "z", torch.float32, (F, L_)), _arg(err, "err", torch.int32, (1,)),
+        _arg(out.get("norm"), "norm", torch.float32, (L_, N)), _arg(D, "D", torch.int32, (F, L_, E)),
+        _arg(tokens, "tokens", torch.int32, (F, L_)), _arg(b, "balance", torch.float32, (F, L_)),
+        _arg(z, "z", torch.float32, (F, L_)), _arg(err, "err", torch.int32, (1,)),
         _dptr(ws) if balance else None, ws.numel() if balance else 0, _stream())
     _check("tacg_route", st)
     out["err"] = err
@@ -560,15 +573,13 @@ def route_backward(logits: torch.Tensor, trace: torch.Tensor, norm: torch.Tensor
         with torch.cuda.stream(stream):
             return route_backward(logits, trace, norm, fam_off, D, tokens, grad_gate, grad_balance, grad_z, score, renorm,
                                   scale, out)
-    ptr, dtype, s_layer, s_token = _logits(logits)
-    L_, N, E = logits.shape
+    ptr, dtype, s_layer, s_token, (L_, N, E) = _logits(logits)
     k = _trace_dims(trace)[2]
-    off = _segments(fam_off, N)
-    F = off.size - 1
+    off, F = _segments(fam_off, N)
     if out is None:
         out = torch.empty((L_, N, E), dtype=logits.dtype, device=logits.device)
-    st = lib().tacg_route_backward(
-        ptr, dtype, s_layer, s_token, N, L_, k, E, _hptr(off), F, _score(score), 1 if renorm else 0, float(scale),
+    st = (_lib or lib()).tacg_route_backward(
+        ptr, dtype, s_layer, s_token, N, L_, k, E, off, F, _score(score), 1 if renorm else 0, float(scale),
         _arg(trace, "trace", torch.int16, (L_, N, k)), _arg(norm, "norm", torch.float32, (L_, N)),
         _arg(D, "D", torch.int32, (F, L_, E)), _arg(tokens, "tokens", torch.int32, (F, L_)),
         _arg(grad_gate, "grad_gate", torch.float32, (L_, N, k)),
@@ -629,10 +640,11 @@ def expert_q4(x: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, scales: torch
     if x.dtype not in (torch.bfloat16, torch.float16) or not x.is_cuda:
         raise ValueError(f"x: expected a bfloat16 or float16 device tensor, got {x.dtype}")
     T, k = ids.shape
-    K = x.shape[-1]
-    if tuple(x.shape) not in ((T, K), (T, k, K)):
-        raise ValueError(f"x: expected [{T}][K] or [{T}][{k}][K], got {tuple(x.shape)}")
-    if x.stride(-1) != 1 and K > 1:
+    shape, stride = x.shape, x.stride()
+    K = shape[-1]
+    if shape != (T, K) and shape != (T, k, K):
+        raise ValueError(f"x: expected [{T}][K] or [{T}][{k}][K], got {tuple(shape)}")
+    if stride[-1] != 1 and K > 1:
         raise ValueError("x: the values of a row must be contiguous")
     if q.dim() != 3 or group < 1:
         raise ValueError(f"q: expected [H][N][bytes] and a positive group, got {tuple(q.shape)}, {group}")
@@ -643,13 +655,14 @@ def expert_q4(x: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, scales: torch
         shape = {"each": (T, k, N), "glu": (T, k, N // 2), "sum": (T, N)}[mode]
         out = torch.empty(shape, dtype=x.dtype, device=x.device)
     code = Q4_MODES[mode]
-    need = lib().tacg_expert_q4_workspace_bytes(T, k, E, N, K, code)
+    C = _lib or lib()
+    need = C.tacg_expert_q4_workspace_bytes(T, k, E, N, K, code) if code == 2 else 0  # only sums of many pairs need one
     if need and (ws is None or ws.numel() < need):
         ws = workspace(need, x.device)
     if err is None:
         err = _err_tensor(x.device)
-    st = lib().tacg_expert_q4(
-        x.data_ptr(), DTYPES[x.dtype], x.stride(0), x.stride(1) if x.dim() == 3 else 0, T, k, E, _dptr(ids),
+    st = C.tacg_expert_q4(
+        x.data_ptr(), DTYPES[x.dtype], stride[0], stride[1] if len(stride) == 3 else 0, T, k, E, _dptr(ids),
         _arg(slot_of_expert, "slot_of_expert", torch.int32, (E,)), H,
         _arg(q, "q", torch.uint8, (H, N, -(-K // 32) * 16)), _arg(scales, "scales", x.dtype, width),
         _arg(zeros, "zeros", torch.uint8, width), group, N, K, code, _arg(gate, "gate", torch.float32, (T, k)),

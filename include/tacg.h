@@ -377,7 +377,7 @@ int tacg_q4_pack(const void* w, int32_t dtype, int64_t n_rows, int32_t n_cols, i
  * TACG_Q4_SUM).  Products are exact in the levels, sums are held in 32 bits, and the result is rounded once; it does not depend on
  * the order of execution.  Data errors: TACG_ERR_ID_RANGE (id >= E or < -1), TACG_ERR_TABLE (h >= n_held); such slots are
  * taken as served elsewhere.  workspace: tacg_expert_q4_workspace_bytes(...) bytes (NULL where that is 0).
- * n_rows, n_cols <= TACG_MAX_WIDTH; T * k < 2^28.
+ * n_rows, n_cols <= TACG_MAX_WIDTH; T * k < 2^27.
  */
 int tacg_expert_q4(const void* x, int32_t dtype, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
                    int32_t top_k, int32_t n_experts, const int16_t* ids, const int32_t* slot_of_expert_or_null,

@@ -437,7 +437,7 @@ int tacg_expert_q4(const void* x, int32_t dtype, int64_t stride_token, int64_t s
   if (mode == TACG_Q4_SUM && gate_or_null == nullptr && n_tokens > 0) return TACG_E_INVAL;
   if (!is_group(group) || n_rows > TACG_MAX_WIDTH || n_cols > TACG_MAX_WIDTH || n_held > TACG_MAX_EXPERTS)
     return TACG_E_UNSUPPORTED;
-  if (n_tokens >= (int64_t(1) << 28) / top_k) return TACG_E_UNSUPPORTED;
+  if (n_tokens >= (int64_t(1) << 27) / top_k) return TACG_E_UNSUPPORTED;
   if (n_held > 0 && (q == nullptr || scales == nullptr || !aligned(q, 16) || !aligned(scales, 2))) return TACG_E_INVAL;
   if (n_tokens == 0) return TACG_OK;
   if (x == nullptr || !aligned(x, 2) || ids == nullptr || out == nullptr || !aligned(out, 2)) return TACG_E_INVAL;

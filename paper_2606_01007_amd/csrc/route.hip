@@ -7,18 +7,21 @@
 //   balance = E / (k T^2) sum_e D_e M_e,   z = 1/T sum_t lse_t^2.
 //
 // route_main: one pass over the logits.  Selection in a row:
-//   * a lane's elements fall into up to eight groups; the k-th largest (4th, 8th or 16th, by the kernel's variant) of the row's group maxima,
-//     found by sorting networks within and merges across the lanes, is a lower bound of the k-th largest logit that few more than k
-//     elements reach;
+//   * a lane's elements fall into up to eight groups; the k-th largest (4th, 8th or 16th, by the kernel's variant) of the row's group
+//     maxima, found by sorting networks within and merges across the lanes, is a lower bound of the k-th largest logit that few
+//     more than k elements reach;
 //   * those elements' values, with the id below the value's last bit (32-bit value and id in a 64-bit float), go to a list in LDS;
 //   * the place of each is the number of larger ones in the list.
-//   A row with more such elements than the list holds (many equal ones) is selected by k passes over the registers instead.
+//   A row with more such elements than the list holds (many equal ones) is selected by k passes over it instead.  (k passes for every
+//   row: 966 us where this takes 140, 58 layers of 8155 rows of 256 in 32 bits with sigmoid scores, counts and loss.)
 //   A workgroup takes a run of rows of one segment; its sums of s' (32 bits over a run, then 64), counts, rows and squares go to a
 //   slot of the workspace, and route_reduce adds a segment's slots in order in 64 bits, so that results do not depend on the
-//   order of execution.
-// route_back: one pass over logits and gradient; with c = d loss / d s' (a constant of the
-//   segment) and u the gradient of the scores through the gates, softmax: dx = s (c + u - sum s (c + u) + 2 gz lse / T).
-//   u has k entries a row: they are laid into a row of LDS, where each lane reads its own experts' back.
+//   order of execution.  Bound by instruction issue with counts and loss (about 880 vector instructions per eight rows of 256, VALU
+//   busy 0.7 of the time, 3.6 TB/s); the selection alone is near memory (48 x 4101 rows of 128: 27 us, 4.1 TB/s).
+// route_back: one pass over logits and gradient; with c = d loss / d s' (a constant of the segment) and u the gradient of the scores
+//   through the gates, softmax: dx = s (c + u - sum s (c + u) + 2 gz lse / T).  u has k entries a row: they are laid into a row of LDS,
+//   where each lane reads its own experts' back.  The softmax is computed again, from differences to the row's largest.  Bound by memory:
+//   58 layers of 8155 rows of 256 in 228 us, 4.4 TB/s read and written (a copy reaches 4.8).
 #include <algorithm>
 #include <cfloat>
 #include <cmath>

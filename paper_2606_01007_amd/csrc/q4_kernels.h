@@ -16,7 +16,8 @@
 //   2048 x 4096, top-8, gated: 281 us, 4.0 TB/s of weights (the same loads without the products: 253; a copy reaches 4.8 TB/s); bound
 //   by the latency of a step (LDS, products, barrier) that two waves a SIMD do not quite hide.  32 tokens through 128 experts
 //   of 1536 x 2048: 63 us, 3.1 TB/s, where a workgroup has eight steps in all.  A second step of weights in flight cost more in
-//   registers than it gave (77 and 331 us).
+//   registers than it gave (77 and 331 us).  Where experts and columns alone leave processors idle, several workgroups share an
+//   expert's tokens: a token's place in its tile, and so its bits, stay the same.
 // q4_few: few pairs.  A workgroup takes 16 weight rows (gated: 16 pairs of them) of the expert of one pair, or, summed, of all experts of a
 //   token; its waves take the steps in turn and add their sums up in LDS, in order.  One token through six experts of 2048 x 2048:
 //   8.2 us; through eight of 4096 x 2048, summed: 11 us, 3.4 TB/s; bound by latency: a wave has one to four steps.
@@ -43,6 +44,7 @@ struct Q4Args {
   int64_t x_token, x_slot;  // strides in elements
   int64_t n_tokens;
   int32_t k, E, H, N, K, group, n_groups, pieces, mode;
+  int32_t shares;           // workgroups that take an expert's tiles of tokens in turn (many pairs)
   const int16_t* ids;
   const int32_t* slot;      // [E] or null
   const uint8_t* q;
@@ -513,7 +515,8 @@ __device__ __forceinline__ void tokens_with_rows(const Q4Args& a, const Rows<T, 
     }
 }
 
-// Many pairs.  grid: (blocks of a workgroup's output columns, held experts and one for the pairs that none serves, runs of kScan pairs).
+// Many pairs.  grid: (blocks of a workgroup's output columns, held experts and one for the pairs that none serves, runs of kScan pairs
+// times shares of the tiles of tokens).
 template <class T, bool GLU, int RT, int TT, int GROUPS, bool ZEROS, bool RAGGED>
 __global__ __launch_bounds__(kThreads, TT == 1 ? 3 : 2) void q4_tiles(Q4Args a) {
   constexpr int kOut = GLU ? RT * 8 : RT * 16;  // output columns of a wave
@@ -524,7 +527,8 @@ __global__ __launch_bounds__(kThreads, TT == 1 ? 3 : 2) void q4_tiles(Q4Args a) 
   __shared__ int total[kWaves];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t pairs = a.n_tokens * a.k, from = static_cast<int64_t>(blockIdx.z) * kScan;
+  const int64_t pairs = a.n_tokens * a.k, from = static_cast<int64_t>(blockIdx.z / a.shares) * kScan;
+  const int share = blockIdx.z % a.shares;
   const int n = static_cast<int>(pairs - from < kScan ? pairs - from : kScan);
   for (int e = tid; e < a.E; e += kThreads) place[e] = static_cast<int16_t>(place_of(a, e));
   const int h = static_cast<int>(blockIdx.y) < a.H ? static_cast<int>(blockIdx.y) : -1;
@@ -534,13 +538,18 @@ __global__ __launch_bounds__(kThreads, TT == 1 ? 3 : 2) void q4_tiles(Q4Args a) 
   const int count = n <= kThreads * 8 ? list_pairs<1>(a, from, n, h, place, list, total)
                                       : list_pairs<2>(a, from, n, h, place, list, total);
   if (h < 0) {
-    if (blockIdx.x == 0)
+    if (blockIdx.x == 0 && share == 0)
       for (int i = tid; i < n; i += kThreads) report(a, look_up(a, place, a.ids[from + i]));
     if (a.mode == TACG_Q4_SUM) return;
-    for (int64_t i = tid; i < static_cast<int64_t>(count) * kWidth; i += kThreads) {
-      const int c = column + static_cast<int>(i % kWidth);
-      if (c < width) static_cast<T*>(a.out)[(from + list[i / kWidth]) * width + c] = static_cast<T>(0.0f);
-    }
+    auto clear = [&](auto value) {  // three of four of 4096 pairs of 1024 columns: 16 bytes at a time 16.5 us a call, one value at a time 57
+      constexpr int kEach = sizeof(value) / sizeof(T), kRow = kWidth / kEach;
+      for (int i = share * kThreads + tid; i < count * kRow; i += a.shares * kThreads) {
+        const int c = column + i % kRow * kEach;
+        if (c < width) *reinterpret_cast<decltype(value)*>(static_cast<T*>(a.out) + (from + list[i / kRow]) * width + c) = value;
+      }
+    };
+    if (width % 8 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0) clear(uint4v{0, 0, 0, 0});
+    else clear(static_cast<T>(0.0f));
     return;
   }
   Rows<T, RT> rows = rows_of<T, RT>(a, h);
@@ -550,7 +559,7 @@ __global__ __launch_bounds__(kThreads, TT == 1 ? 3 : 2) void q4_tiles(Q4Args a) 
     v = v < width ? v : width - 1;
     rows.at[r] = v + (GLU && r >= RT / 2 ? width : 0);
   }
-  for (int base = 0; base < count; base += 16 * TT) {
+  for (int base = share * 16 * TT; base < count; base += a.shares * 16 * TT) {
     const int left = count - base;
     if (TT == 2 && left > 16) tokens_with_rows<T, GLU, RT, TT, GROUPS, ZEROS, RAGGED>(a, rows, list, from, base, count, column, held);
     else if (left > 2) tokens_with_rows<T, GLU, RT, 1, GROUPS, ZEROS, RAGGED>(a, rows, list, from, base, count, column, held);
@@ -697,11 +706,22 @@ void by_weights(const Q4Args& a, Launch launch) {
   else with(std::integral_constant<int, 1>());
 }
 
+// Shares of an expert's tiles of tokens: a grid that leaves processors idle spreads them, up to 512 workgroups, and as many as twice
+// the mean of an expert's tokens fills.  One share against this rule in us, 512 tokens: each, 8 experts of 1024 x 2048, top-2:
+// 45.7 / 22.6; gated, 2048 x 2048: 59.8 / 29.2 (a limit of 256: 38.8, of 1024: 32.4), 4096 x 2048: 62.2 / 42.6 (61.1, 47.9).
+inline int32_t q4_shares(int64_t workgroups, int64_t pairs, int32_t n_experts, int32_t tokens) {
+  const int64_t fills = 512 / workgroups, tiles = (2 * pairs / n_experts + tokens - 1) / tokens;
+  const int64_t shares = fills < tiles ? fills : tiles;
+  return static_cast<int32_t>(shares < 1 ? 1 : shares);
+}
+
 template <class T, bool RAGGED, bool GLU, int RT, int TT>
-void start_tiles(const Q4Args& a, hipStream_t stream) {
+void start_tiles(Q4Args a, hipStream_t stream) {
   const int64_t pairs = a.n_tokens * a.k;
   const int width = GLU ? a.N / 2 : a.N, block = (GLU ? RT * 8 : RT * 16) * kWaves;
-  const dim3 grid((width + block - 1) / block, a.H + 1, static_cast<uint32_t>((pairs + kScan - 1) / kScan));
+  const int64_t runs = (pairs + kScan - 1) / kScan, columns = (width + block - 1) / block;
+  a.shares = q4_shares(columns * (a.H > 0 ? a.H : 1) * runs, pairs < kScan ? pairs : kScan, a.E, 16 * TT);
+  const dim3 grid(static_cast<uint32_t>(columns), a.H + 1, static_cast<uint32_t>(runs * a.shares));
   by_weights(a, [&](auto groups, auto zeros) {
     q4_tiles<T, GLU, RT, TT, groups.value, zeros.value, RAGGED><<<grid, kThreads, 0, stream>>>(a);
   });

@@ -1,5 +1,7 @@
 """The experts' products with many pairs: every number of weight rows a wave and of token tiles that the sizes choose, lists over several
 runs of pairs, and pairs at the rules' edges.  Tolerances as in test_gpu_q4."""
+import math
+
 import pytest
 import torch
 
@@ -94,3 +96,36 @@ def test_a_share_over_several_runs_of_pairs(mode):
     ids = _routed(8, T, E, k, unused=0.1)
     x, gate = _inputs(8, T, k, K, mode, torch.bfloat16)
     _check(_run(x, ids, w, group, mode, E, slot=slot, gate=gate), x, ids, w, group, mode, slot=slot, gate=gate)
+
+
+@pytest.mark.parametrize("mode", ["each", "glu", "sum"])
+@pytest.mark.parametrize("N, K", [(256, 320), (248, 300), (70, 512), (2, 256)])
+@pytest.mark.parametrize("held", [0, 1, 3, 5])
+def test_many_tokens_of_few_experts(mode, N, K, held):
+    """Small grids, whose experts' tiles of tokens go to several workgroups; rows without a held expert are zero, into memory that was
+    not, at an address that holds 16 bytes' alignment and at one that does not."""
+    T, E, k, group = 333, 5, 2, 64
+    slot = torch.tensor([3, -1, 0, 2, 1] if held == 5 else [v if v < held else -1 for v in (2, 4, 0, 3, 1)], dtype=torch.int32)
+    w = _weights(N + held, held, N, K, group, torch.bfloat16, held == 3)
+    ids = _routed(held, T, E, k, unused=0.05)
+    x, gate = _inputs(held, T, k, K, mode, torch.bfloat16)
+    shape = {"each": (T, k, N), "glu": (T, k, N // 2), "sum": (T, N)}[mode]
+    size = math.prod(shape)
+    for skip in (0, 1):
+        room = torch.full((skip + size + 8,), 7.0, dtype=torch.bfloat16, device="cuda")
+        out = room[skip:skip + size].view(shape)
+        _run(x, ids, w, group, mode, E, slot=slot, gate=gate, out=out)
+        _check(out, x, ids, w, group, mode, slot=slot, gate=gate)
+        assert torch.all(room[:skip] == 7) and torch.all(room[skip + size:] == 7)
+
+
+def test_a_row_has_the_same_bits_however_many_workgroups_share_its_expert():
+    """The tiles' places do not change with the number of workgroups: a call of fewer rows of weights, with more workgroups an expert, gives
+    the same bits for these rows."""
+    T, E, k, K, group = 400, 6, 2, 512, 64
+    q, s, z = _weights(3, E, 2048, K, group, torch.float16, True)
+    ids = _routed(3, T, E, k)
+    x, _ = _inputs(3, T, k, K, "each", torch.float16)
+    whole = _run(x, ids, (q, s, z), group, "each", E)
+    part = _run(x, ids, tuple(v[:, :64].contiguous() for v in (q, s, z)), group, "each", E)
+    assert torch.equal(part, whole[..., :64])

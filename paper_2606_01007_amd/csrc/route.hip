@@ -804,7 +804,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_back(BackArgs a) {
     float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      p[i] = a.softmax ? p[i] * inverse : sigmoid(p[i]);
+      p[i] = a.softmax ? p[i] * inverse : live ? sigmoid(p[i]) : 0.0f;  // a row that is not routed may hold a NaN
       dot += p[i] * c[i];
     }
     dot = row_sum(dot);

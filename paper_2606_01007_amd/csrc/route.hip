@@ -19,9 +19,9 @@
 //   order of execution.  Bound by instruction issue with counts and loss (about 880 vector instructions per eight rows of 256, VALU
 //   busy 0.7 of the time, 3.6 TB/s); the selection alone is near memory (48 x 4101 rows of 128: 27 us, 4.1 TB/s).
 // route_back: one pass over logits and gradient; with c = d loss / d s' (a constant of the segment) and u the gradient of the scores
-//   through the gates, softmax: dx = s (c + u - sum s (c + u) + 2 gz lse / T).  u has k entries a row: they are laid into a row of LDS,
-//   where each lane reads its own experts' back.  The softmax is computed again, from differences to the row's largest.  Bound by memory:
-//   58 layers of 8155 rows of 256 in 228 us, 4.4 TB/s read and written (a copy reaches 4.8).
+//   through the gates, softmax: dx = s (c + u - sum s (c + u) + 2 gz lse / T), sigmoid: dx = (1 - s) (s' (c - sum s' c) + u s).  u s has
+//   k entries a row: they are laid into a row of LDS, where each lane reads its own experts' back.  The softmax is computed again, from
+//   differences to the row's largest.  Bound by memory: 58 layers of 8155 rows of 256 in 228 us, 4.4 TB/s read and written (a copy reaches 4.8).
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -542,15 +542,15 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
 #pragma unroll
       for (int q = 0; q < KS; ++q) w[q] = sigmoid(w[q]);
     }
-    float factor = a.scale;
+    float factor = 1.0f;
     if (a.renorm) {
       float part = 0.0f;
 #pragma unroll
       for (int q = 0; q < KS; ++q) part += w[q];
       part = row_sum(part);
-      factor = part > 0.0f ? a.scale / part : 0.0f;
+      factor = part > 0.0f ? 1.0f / part : 0.0f;
     } else if (a.softmax) {
-      factor = a.scale * inverse;
+      factor = inverse;
     }
     const int64_t at = static_cast<int64_t>(l) * a.n_tokens + t;
     if (in) {
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
         const int j = sub + q * kRowLanes;
         if (j < k) {
           a.trace[at * k + j] = static_cast<int16_t>(id[q]);
-          a.gate[at * k + j] = w[q] * factor;
+          a.gate[at * k + j] = w[q] * factor * a.scale;  // the share first: factor * scale may be more than 32 bits hold
           if (BAL && id[q] >= 0) atomicAdd(&count[id[q]], 1u);
         }
       }
@@ -701,7 +701,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_reduce(ReduceArgs a) {
 template <class T, int CH, int KS>
 __global__ __launch_bounds__(kRouteThreads) void route_back(BackArgs a) {
   constexpr int V = kChunk<T>, M = CH * V, kStride = M * kRowLanes + 32;
-  __shared__ float sparse[kRowsPerPass][kStride];  // gradient of the scores of a row's selected experts, else 0
+  __shared__ float sparse[kRowsPerPass][kStride];  // u s of a row's selected experts, else 0
   const int tid = threadIdx.x, lane = tid & 63, sub = lane & (kRowLanes - 1);
   const int l = blockIdx.y;
   const Run run = run_of(a, blockIdx.x);
@@ -761,7 +761,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_back(BackArgs a) {
       total = row_sum(total);
       inverse = live ? 1.0f / total : 0.0f;
     }
-    // scores of the selected, and the gradient through the gates
+    // scores s of the selected, and the gradient u of the scores through the gates, times s.  Sums of scores are divided by first: shares are
+    // numbers up to 1, while a reciprocal or a score alone, multiplied, may leave the range of 32 bits
     if (a.softmax) {
       float high = top;
       if (a.renorm) {
@@ -776,25 +777,22 @@ __global__ __launch_bounds__(kRouteThreads) void route_back(BackArgs a) {
 #pragma unroll
       for (int q = 0; q < KS; ++q) s[q] = id[q] >= 0 ? sigmoid(s[q]) : 0.0f;
     }
-    float su = 0.0f;  // softmax without renormalisation: sum s u
+    float su = 0.0f;  // softmax without renormalisation: sum of u s
     if (a.renorm) {
       float part = 0.0f, mean = 0.0f;
 #pragma unroll
-      for (int q = 0; q < KS; ++q) part += s[q], mean += s[q] * u[q];
+      for (int q = 0; q < KS; ++q) part += s[q];
       part = row_sum(part);
       const float inv = part > 0.0f ? 1.0f / part : 0.0f;
-      mean = row_sum(mean) * inv;
-      // softmax: straight to the logits, gate (g - mean); sigmoid: to the score
 #pragma unroll
-      for (int q = 0; q < KS; ++q) u[q] = a.scale * inv * (u[q] - mean) * (a.softmax ? s[q] : 1.0f);
+      for (int q = 0; q < KS; ++q) s[q] *= inv, mean += s[q] * u[q];
+      mean = row_sum(mean);
+#pragma unroll
+      for (int q = 0; q < KS; ++q) u[q] = a.scale * (u[q] - mean) * s[q];
     } else {
 #pragma unroll
-      for (int q = 0; q < KS; ++q) u[q] *= a.scale, su += s[q] * u[q];
-      if (a.softmax) {
-        su = row_sum(su);
-#pragma unroll
-        for (int q = 0; q < KS; ++q) u[q] *= s[q];
-      }
+      for (int q = 0; q < KS; ++q) u[q] = a.scale * u[q] * s[q], su += u[q];
+      if (a.softmax) su = row_sum(su);
     }
 #pragma unroll
     for (int q = 0; q < KS; ++q)
@@ -802,27 +800,26 @@ __global__ __launch_bounds__(kRouteThreads) void route_back(BackArgs a) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     // all experts of the row
     float dot = 0.0f;
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-      p[i] = a.softmax ? p[i] * inverse : live ? sigmoid(p[i]) : 0.0f;  // a row that is not routed may hold a NaN
-      dot += p[i] * c[i];
-    }
-    dot = row_sum(dot);
     if (a.softmax) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        p[i] *= inverse;
+        dot += p[i] * c[i];
+      }
+      dot = row_sum(dot);
       const float sub_all = (live ? zc * norm : 0.0f) - dot - (a.renorm ? 0.0f : su);
 #pragma unroll
-      for (int i = 0; i < M; ++i) {
-        const int e = ((i / V) * kRowLanes + sub) * V + i % V;
-        p[i] = p[i] * (c[i] + sub_all) + mine[e];
-      }
+      for (int i = 0; i < M; ++i) p[i] = p[i] * (c[i] + sub_all) + mine[element<T, CH>(i, sub)];
     } else {
       const float inv = live ? 1.0f / norm : 0.0f;
-      dot *= inv;
 #pragma unroll
       for (int i = 0; i < M; ++i) {
-        const int e = ((i / V) * kRowLanes + sub) * V + i % V;
-        p[i] = p[i] * (1.0f - p[i]) * ((c[i] - dot) * inv + mine[e]);
+        p[i] = live ? sigmoid(p[i]) : 0.0f;  // a row that is not routed may hold a NaN
+        dot += p[i] * inv * c[i];
       }
+      dot = row_sum(dot);
+#pragma unroll
+      for (int i = 0; i < M; ++i) p[i] = (1.0f - p[i]) * (p[i] * inv * (c[i] - dot) + mine[element<T, CH>(i, sub)]);
     }
     if (in) store_row<T, CH>(static_cast<T*>(a.grad) + at * E, sub, E, a.vec, p);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -22,6 +22,7 @@ class _Route(torch.autograd.Function):
         kept.update(r)
         ctx.save_for_backward(logits, r["trace"], r["norm"], r["D"], r["tokens"])
         ctx.how = (fam_off, score, renorm, scale)
+        ctx.set_materialize_grads(False)  # an output without a gradient is left out, not read as zeros
         z = r.get("z")
         return r["gate"], r["balance"], torch.zeros_like(r["balance"]) if z is None else z
 

@@ -4,13 +4,15 @@
     loss = task_loss(gate, r["trace"]) + 0.01 * balance.mean() + 0.001 * z.mean()
     loss.backward()                                      # logits.grad through tacg_route_backward
 
-The selection and the counts are constants of the gradient, as usual for these losses.
+The selection and the counts are constants of the gradient, as usual for these losses.  There is no second derivative: asking for one
+raises.
 """
 from __future__ import annotations
 
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import route, route_backward
 
@@ -27,6 +29,7 @@ class _Route(torch.autograd.Function):
         return r["gate"], r["balance"], torch.zeros_like(r["balance"]) if z is None else z
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_gate, grad_balance, grad_z):
         logits, trace, norm, D, tokens = ctx.saved_tensors
         fam_off, score, renorm, scale = ctx.how

@@ -43,3 +43,12 @@ def test_outputs_that_no_loss_uses_have_no_gradient(calls, score, used):
     given = {n for n in ("gate", "balance", "z") if calls[0]["grad_" + n] is not None}
     assert given == ({used} if (score, used) != ("sigmoid", "z") else set())
     assert torch.equal(x.grad, torch.ones_like(x))
+
+
+def test_a_second_derivative_is_refused(calls):
+    """The backward pass runs outside automatic differentiation: a second derivative through it would lack the router's part."""
+    x = _logits()
+    gate, balance, _, _ = training.balanced_route(x, 2, [0, 6])
+    (first,) = torch.autograd.grad((gate * x[:, :, :2]).sum() + balance.sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        first.sum().backward()

@@ -14,7 +14,7 @@ from typing import Optional
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import route, route_backward
+from . import _fam_off, route, route_backward
 
 
 class _Route(torch.autograd.Function):
@@ -45,5 +45,7 @@ def balanced_route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = 
     """(gate [L][N][k], balance [F][L], z [F][L], the dict of `route`): gate, balance and z are differentiable with respect to the
     logits.  z is 0 for sigmoid scores, which have none."""
     kept: dict = {}
+    if fam_off is not None:
+        fam_off = _fam_off(fam_off).tolist()  # a copy: the backward pass takes the same families, whatever becomes of the caller's
     gate, balance, z = _Route.apply(logits, top_k, fam_off, score, bias, renorm, scale, kept)
     return gate, balance, z, kept

@@ -1,5 +1,6 @@
 """The differentiable router's calls (CPU only): what its backward pass hands to `route_backward`, with both calls replaced by stand-ins
 that note their arguments and compute gate = logits of the first k experts, balance and z = sums of logits."""
+import numpy as np
 import pytest
 import torch
 
@@ -52,3 +53,13 @@ def test_a_second_derivative_is_refused(calls):
     (first,) = torch.autograd.grad((gate * x[:, :, :2]).sum() + balance.sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         first.sum().backward()
+
+
+@pytest.mark.parametrize("make", [list, np.array, torch.tensor])
+def test_the_families_are_those_of_the_forward_call(calls, make):
+    x = _logits()
+    off = make([0, 2, 6])
+    gate, balance, z, _ = training.balanced_route(x, 2, off)
+    off[1] = 5
+    (balance.sum() + z.sum()).backward()
+    assert [int(v) for v in calls[0]["fam_off"]] == [0, 2, 6]

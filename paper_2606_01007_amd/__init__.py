@@ -518,7 +518,8 @@ def route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = "softmax"
 
     dict(trace int16 [L][N][k], gate float32 [L][N][k], err), with want_norm or balance also norm float32 [L][N], and with
     balance D [F][L][E], tokens [F][L] (uint32 bits), balance float32 [F][L] and, for softmax scores, z float32 [F][L].
-    Masked experts have the logit -inf; where fewer than k are left the trace holds -1 and the gate 0."""
+    Masked experts have the logit -inf; where fewer than k are left the trace holds -1 and the gate 0.  A NaN or +inf logit sets
+    ERR_VALUE in err."""
     if stream is not None:  # all of the call, its buffers too, on that stream
         with torch.cuda.stream(stream):
             return route(logits, top_k, fam_off, score, bias, renorm, scale, balance, want_norm, ws, err, out)
@@ -592,7 +593,8 @@ def route_backward(logits: torch.Tensor, trace: torch.Tensor, norm: torch.Tensor
 def q4_pack(weight: torch.Tensor, group: int = 128, symmetric: bool = True, scale_dtype: Optional[torch.dtype] = None,
             err: Optional[torch.Tensor] = None, stream=None):
     """Weights [H][N][K] in 4 bits (tacg_q4_pack): q uint8 [H][N][ceil(K / 32) * 16], scales [H][N][ceil(K / group)] in
-    scale_dtype (default: the weights' type, bfloat16 for float32 ones) and zeros (uint8, as scales) or None."""
+    scale_dtype (default: the weights' type, bfloat16 for float32 ones) and zeros (uint8, as scales) or None.  Weights or scales that
+    are not finite set ERR_VALUE in `err` (int32 [1], 0 at first): without one nothing reports them."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return q4_pack(weight, group, symmetric, scale_dtype, err)
@@ -629,7 +631,9 @@ def expert_q4(x: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, scales: torch
     x [T][K], or [T][k][K] where every slot has its own; rows contiguous, in bfloat16 or float16 as scales.  ids int16 [T][k]: the
     routed experts (a layer of a trace).  q, scales, zeros: the n_held experts of this GPU (q4_pack); slot_of_expert int32 [E] gives
     each expert's place among them, below 0 for an expert held elsewhere (None: all are held, in order).  mode: "each" -> [T][k][N],
-    "glu" -> [T][k][N / 2], "sum" (needs gate float32 [T][k]) -> [T][N].  Slots that are not served here add 0."""
+    "glu" -> [T][k][N / 2], "sum" (needs gate float32 [T][k]) -> [T][N].  Slots that are not served here add 0.  So do ids out of
+    range and bad entries of slot_of_expert, which set ERR_ID_RANGE and ERR_TABLE in `err` (int32 [1], 0 at first; the calls of a
+    program can share one): without one nothing reports them."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return expert_q4(x, ids, q, scales, zeros, group, mode, n_experts, slot_of_expert, gate, ws, err, out)

@@ -360,6 +360,7 @@ int tacg_route_backward(const void* logits, int32_t dtype, int64_t stride_layer,
  *                  level = clamp(round(W / scale) + zero, 0, 15)
  * per group, with the scale as rounded to its type, in 32-bit arithmetic, halves to even; a group whose scale is 0 gets the
  * level 8 (and zero 8).  Data errors: TACG_ERR_VALUE (a weight that is not finite, or a scale that its type cannot hold).
+ * n_rows <= 2^26, n_cols <= TACG_MAX_WIDTH, n_rows * G * group <= 2^37 - 2^13 (else TACG_E_UNSUPPORTED).
  */
 int tacg_q4_pack(const void* w, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride, int32_t group,
                  int32_t scale_dtype, uint8_t* q, void* scales, uint8_t* zeros_or_null, uint32_t* d_err,

@@ -410,6 +410,8 @@ int tacg_q4_pack(const void* w, int32_t dtype, int64_t n_rows, int32_t n_cols, i
   if (dtype != TACG_F32 && !is_half(dtype)) return TACG_E_INVAL;
   if (!is_half(scale_dtype) || n_rows < 0 || n_cols < 1 || row_stride < 0 || d_err == nullptr) return TACG_E_INVAL;
   if (!is_group(group) || n_cols > TACG_MAX_WIDTH || n_rows > (int64_t(1) << 26)) return TACG_E_UNSUPPORTED;
+  // a launch holds fewer than 2^32 threads, here a thread per 32 columns of whole groups and 256 to a workgroup
+  if (n_rows * ((n_cols + group - 1) / group) * (group / 32) > (int64_t(1) << 32) - 256) return TACG_E_UNSUPPORTED;
   if (n_rows == 0) return TACG_OK;
   if (w == nullptr || !aligned(w, dtype == TACG_F32 ? 4 : 2) || q == nullptr || !aligned(q, 16)) return TACG_E_INVAL;
   if (scales == nullptr || !aligned(scales, 2)) return TACG_E_INVAL;

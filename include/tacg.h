@@ -319,8 +319,9 @@ int tacg_jain(const uint32_t* load, int32_t n_place, int32_t n_layers, int32_t n
  *   D[f][l][e]     = number of those rows whose selection contains e (as tacg_coact_build counts the trace)
  *   balance[f][l]  = sum_e (E / (k T) D_e) (1/T sum_t s'_e(t))         z[f][l] = 1/T sum_t norm_t^2
  * and 0 where T = 0.  z is optional and for TACG_SOFTMAX (else TACG_E_INVAL).  norm[L][N] is optional, 0 (sigmoid) or -inf
- * (softmax) for a row without an available expert.  Scores and sums are held in 32 bits (a sigmoid below 2^-126 is 0), sums over tokens
- * in 64; results do not depend on the order of execution.  A trace with unused slots (-1) is not one that the trace passes above take.
+ * (softmax) for a row without an available expert.  Scores and sums over experts are held in 32 bits (a sigmoid below 2^-126 is 0), and so
+ * are sums over the tokens that one workgroup takes, up to 512; those are added in 64 bits, in order, so that results do not depend on
+ * the order of execution.  A trace with unused slots (-1) is not one that the trace passes above take.
  * Outputs: int16 trace[L][N][k] (2-byte aligned), float gate[L][N][k], float norm[L][N], uint32 D[F][L][E], uint32 tokens[F][L],
  * float balance[F][L], float z[F][L].  Data errors: TACG_ERR_VALUE (a NaN or +inf logit; that row counts as one without
  * available experts).  workspace: tacg_route_workspace_bytes(...) bytes with the balance outputs, else may be NULL.

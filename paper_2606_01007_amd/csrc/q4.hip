@@ -1,6 +1,7 @@
 // Weights in 4 bits: packing, and the host side of the experts' products (kernels: q4_kernels.h).
 //
-// q4_pack_kernel: levels, scales and zeros of a weight matrix, a lane per 32 columns (16 bytes of levels).
+// q4_pack_kernel: levels, scales and zeros of a weight matrix, a lane per 32 columns (16 bytes of levels), read one by one; done once
+//   per weight.  64 matrices of 2048 x 2048 in bfloat16: 548 us, a quarter of what a copy reaches; bound by its loads of 2 bytes.
 // q4_combine: sums the 32-bit products of many pairs over the slots of a token.
 #include <algorithm>
 #include <cmath>

@@ -30,9 +30,13 @@
 namespace tacg {
 
 // Few pairs: most have an expert of their own, so a workgroup per pair (or token) leaves little to share and wastes none on experts
-// without tokens.  Measured, few against many in us: gated, 128 experts of 1536 x 2048, top-8: 20.5 / 25.6 at 4 tokens, 35.9 / 29.9
-// at 8; 60 experts, top-4: 12.4 / 20.4 at 4, 20.2 / 23.1 at 8, 33.6 / 25.1 at 16.  Summed (2048 x 1024): 30.4 / 32.4 at 16 tokens
-// of 128 experts, 56.4 / 37.1 at 32; 18.2 / 21.3 at 16 of 60, 33.0 / 21.9 at 32.
+// without tokens.  Measured, few against many in us: gated, 128 experts of 1536 x 2048, top-8: 20.1 / 30.4 at 4 tokens, 29.9 / 30.4
+// at 6, 36.2 / 30.7 at 8; 60 experts of 2048 x 2048, top-4: 14.1 / 23.0 at 4, 20.6 / 23.2 at 6, 25.5 / 23.5 at 8.  Each: 22.6 / 30.1,
+// 31.3 / 30.3, 39.4 / 30.9; 16.3 / 23.1, 21.8 / 23.2, 28.1 / 23.6.  Summed (2048 x 1024): 31.3 / 33.7 at 16 tokens of 128 experts,
+// 56.0 / 37.1 at 32; 17.7 / 21.2 at 15 of 60, 17.9 / 21.8 at 16, 32.9 / 22.7 at 32.
+// The rule goes by the pairs alone, so it is not the faster one everywhere: 256 experts of 2048 x 1024, top-8, 8 tokens: gated 37.1 / 26.4, each
+// 44.3 / 26.0; summed, 256 of 4096 x 2048, 32 tokens: 233 / 179.  An expert's pairs go two at a time: 100 pairs that all choose one of
+// 256 experts of 2048 x 2048: gated 122 / 74.6, each 71.8 / 74.3.
 inline bool q4_few_pairs(int64_t pairs, int32_t n_experts, int32_t mode) {
   return mode == TACG_Q4_SUM ? pairs <= n_experts : 5 * pairs <= 2 * static_cast<int64_t>(n_experts);
 }

@@ -379,8 +379,9 @@ int tacg_q4_pack(const void* w, int32_t dtype, int64_t n_rows, int32_t n_cols, i
  * TACG_Q4_SUM).  Products are exact in the levels, sums are held in 32 bits, and the result is rounded once; it does not depend on
  * the order of execution, nor on the values of other tokens (their number may change the order of a sum).  The sums run over levels
  * with an offset of up to 128, which is subtracted again: an x(t, j) with an infinity, or with a group of columns whose |x| sum to
- * 2^120 or more (bfloat16), gives NaN or an infinity in all of that product.  Data errors: TACG_ERR_ID_RANGE (id >= E or < -1), TACG_ERR_TABLE (h >= n_held); such slots are
- * taken as served elsewhere.  workspace: tacg_expert_q4_workspace_bytes(...) bytes (NULL where that is 0).
+ * 2^120 or more (bfloat16), gives NaN or an infinity in all of that product.  Data errors: TACG_ERR_ID_RANGE (id >= E or < -1),
+ * TACG_ERR_TABLE (h >= n_held); such slots are taken as served elsewhere.  workspace: tacg_expert_q4_workspace_bytes(...) bytes (NULL
+ * where that is 0).
  * n_rows, n_cols <= TACG_MAX_WIDTH; T * k < 2^27.
  */
 int tacg_expert_q4(const void* x, int32_t dtype, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,

@@ -56,12 +56,13 @@ extern "C" {
 #define TACG_F32 0
 #define TACG_BF16 1
 #define TACG_F16 2
+#define TACG_I8 3 /* levels of tokens, for tacg_expert_i8 */
 
 /* scores of the router */
 #define TACG_SOFTMAX 0
 #define TACG_SIGMOID 1
 
-/* what tacg_expert_q4 makes of its products */
+/* what tacg_expert_q4 and tacg_expert_i8 make of their products */
 #define TACG_Q4_EACH 0
 #define TACG_Q4_GLU 1
 #define TACG_Q4_SUM 2
@@ -71,10 +72,11 @@ extern "C" {
 #define TACG_MAX_TOPK 16
 #define TACG_MAX_FAMILIES 64
 #define TACG_MAX_GPUS 32
+#define TACG_MAX_GROUPS 32  /* of experts, in a router's selection */
 #define TACG_MAX_SECONDARY 4
 #define TACG_MAX_REPLICATED 16
 #define TACG_MAX_TOP_PAIRS 4096
-#define TACG_MAX_WIDTH 65536 /* rows and columns of an expert's 4-bit weights */
+#define TACG_MAX_WIDTH 65536 /* rows and columns of an expert's weights */
 #define TACG_NOALLOC_SCRATCH_BYTES ((size_t)32 << 20) /* device scratch of the no-allocation entry point */
 
 /*
@@ -336,6 +338,24 @@ int tacg_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t 
 size_t tacg_route_workspace_bytes(int64_t n_tokens, int32_t n_layers, int32_t n_experts, int32_t n_fam);
 
 /*
+ * tacg_route with a selection that groups of experts limit.  Group g holds the experts g * E / n_groups up to those of the next (n_groups
+ * divides E).  With v_e = s_e, or s_e + bias[l][e], a group's score is the sum of the group_best (1 or 2) largest v_e of its
+ * available experts (of one, where it has one); without a bias and with group_best = 1 it is the largest logit.  The top_groups groups of
+ * largest score that have an available expert are kept, ties go to the lower number, and the k experts are chosen among theirs as tacg_route
+ * chooses among all: fewer than k, and -1 in the slots behind, where those groups have fewer.  Scores, norm, counts and losses
+ * are over all available experts, as there.  What 32 bits cannot order is ordered in 64: sums of scores, and scores with a bias, are
+ * compared as 64-bit numbers where they are nearer than 32-bit ones can tell (up to the last eight of their bits for scores with a
+ * bias).  The backward pass is tacg_route_backward.  n_groups = 1 is tacg_route, with its order in 32 bits.
+ * 1 <= top_groups <= n_groups <= TACG_MAX_GROUPS (else TACG_E_UNSUPPORTED for more groups, TACG_E_INVAL otherwise).
+ */
+int tacg_route_grouped(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+                       int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+                       int32_t score, const float* bias_or_null, int32_t renormalise, float scale, int32_t n_groups,
+                       int32_t top_groups, int32_t group_best, int16_t* trace, float* gate, float* norm_or_null,
+                       uint32_t* D_or_null, uint32_t* tokens_or_null, float* balance_or_null, float* z_or_null,
+                       uint32_t* d_err, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Gradient of the router's gates and losses to its logits.  logits, trace, norm, D and tokens are those of tacg_route (selection
  * and counts are constants, as usual for these losses); score, renormalise and scale too.
  *   grad_logits = sum_{l,t,j} grad_gate d gate / d x  +  sum_{f,l} grad_balance d balance / d x  +  grad_z d z / d x
@@ -392,6 +412,47 @@ int tacg_expert_q4(const void* x, int32_t dtype, int64_t stride_token, int64_t s
 
 size_t tacg_expert_q4_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_rows,
                                       int32_t n_cols, int32_t mode);
+
+/*
+ * Products in 8-bit integers, with a scale for each token and for each weight row.  A row of n_cols values v with the largest magnitude m
+ * becomes levels and a scale, in 32 bits:
+ *   level_c = 127 v_c / m, rounded to an integer, halves to even (-127..127; exactly so for 16-bit values)      scale = m / 127
+ * and 0 where m = 0.  A row with a value that is not finite gets the scale NaN and levels 0, and sets TACG_ERR_VALUE.
+ * tacg_token_i8: rows of x, type `dtype`, row_stride elements apart (>= 0) -> q[n_rows][C] (16-byte aligned; C = n_cols rounded up
+ * to 64, 0 past n_cols) and scale[n_rows].
+ * tacg_i8_pack: n_matrices contiguous matrices [n_rows][n_cols] -> scale[matrix][n_rows] and
+ *   q[matrix][ceil(n_rows / 16)][ceil(n_cols / 64)][4][16][16]  (16-byte aligned): the level of row r, column c at
+ *   [r / 16][c / 64][c % 64 / 16][r % 16][c % 16], 0 past n_rows and n_cols.
+ * n_cols <= TACG_MAX_WIDTH, n_rows of a matrix too; n_matrices <= TACG_MAX_EXPERTS; n_rows of tacg_token_i8 < 2^31.
+ */
+int tacg_token_i8(const void* x, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride, int8_t* q, float* scale,
+                  uint32_t* d_err, void* hip_stream);
+int tacg_i8_pack(const void* w, int32_t dtype, int32_t n_matrices, int32_t n_rows, int32_t n_cols, int8_t* q, float* scale,
+                 uint32_t* d_err, void* hip_stream);
+
+/*
+ * Products of tokens with the 8-bit weights of the experts that they are routed to, of those that this GPU holds.  w and w_scale are
+ * n_held matrices of tacg_i8_pack.  ids, slot_of_expert, strides, modes and what is served elsewhere are as in tacg_expert_q4; with
+ * ids NULL every token takes all n_held matrices, slot j the j-th (shared experts: top_k = n_held, slot_of_expert NULL).
+ *   x in TACG_F32, TACG_BF16 or TACG_F16: rounded to levels within the call, as tacg_token_i8 rounds it (x_scale NULL);
+ *   x in TACG_I8: levels of tacg_token_i8 with their scales x_scale, [T] or, with stride_slot > 0, [T][k]; strides are multiples of
+ *     16 and x is 16-byte aligned; a row has n_cols rounded up to 64 readable bytes, of which those past n_cols do not matter.
+ * The modes are those of tacg_expert_q4, with W_h[n] . x = (x_scale * w_scale[h][n]) * sum over c of levels; gate NULL is a gate of 1.
+ * out has type out_dtype (TACG_F32, TACG_BF16, TACG_F16).  Sums over columns are exact, those over slots are held in 32 bits in the order
+ * of the slots, and the result is rounded once: it depends on nothing but its token, its weights and its gates.  A token with a
+ * value that is not finite gives NaN in its products, and sets TACG_ERR_VALUE; other data errors are those of tacg_expert_q4.  Tokens
+ * and weights may be anything else that 32-bit products of the scales can hold.  workspace: tacg_expert_i8_workspace_bytes(...) bytes
+ * (NULL where that is 0).  n_rows, n_cols <= TACG_MAX_WIDTH; n_held <= TACG_MAX_EXPERTS; T * k < 2^27.
+ */
+int tacg_expert_i8(const void* x, int32_t dtype, const float* x_scale_or_null, int64_t stride_token, int64_t stride_slot,
+                   int64_t n_tokens, int32_t top_k, int32_t n_experts, const int16_t* ids_or_null,
+                   const int32_t* slot_of_expert_or_null, int32_t n_held, const int8_t* w, const float* w_scale, int32_t n_rows,
+                   int32_t n_cols, int32_t mode, const float* gate_or_null, void* out, int32_t out_dtype, uint32_t* d_err,
+                   void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* per_slot: whether stride_slot > 0 */
+size_t tacg_expert_i8_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode,
+                                      int32_t dtype, int32_t per_slot);
 
 /* Human-readable text of a status code (static storage). */
 const char* tacg_strerror(int status);

@@ -16,6 +16,8 @@ kernels.  There is no fallback: if the library or the GPU is missing, the calls 
     grad = route_backward(logits, r["trace"], r["norm"], fam_off, D=r["D"], tokens=r["tokens"], grad_balance=g)
     q, scales, zeros = q4_pack(weights, group=128)           # experts in 4 bits
     h = expert_q4(x, trace[l], q, scales, group=128, mode="glu")
+    q, scale = i8_pack(weights)                              # experts in 8 bits, tokens rounded to 8 bits in the call
+    h = expert_i8(x, trace[l], q, scale, mode="glu")
 
 Unsigned 32-bit device outputs are held in torch.int32 tensors (same bits) and unsigned 64-bit ones in
 torch.int64 tensors; `as_u32` converts the former to int64 values.
@@ -42,6 +44,7 @@ NONE = 0xFF
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 SCORES = {"softmax": 0, "sigmoid": 1}
 Q4_MODES = {"each": 0, "glu": 1, "sum": 2}
+I8 = 3
 
 _lock = threading.Lock()
 _lib = None
@@ -101,6 +104,14 @@ def lib():
                                          P, P, sz, P]
             L.tacg_expert_q4_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
             L.tacg_expert_q4_workspace_bytes.restype = sz
+            L.tacg_route_grouped.argtypes = [P, i32, i64, i64, i64, i32, i32, i32, P, i32, i32, P, i32, f32, i32, i32, i32, P,
+                                             P, P, P, P, P, P, P, P, sz, P]
+            L.tacg_token_i8.argtypes = [P, i32, i64, i32, i64, P, P, P, P]
+            L.tacg_i8_pack.argtypes = [P, i32, i32, i32, i32, P, P, P, P]
+            L.tacg_expert_i8.argtypes = [P, i32, P, i64, i64, i64, i32, i32, P, P, i32, P, P, i32, i32, i32, P, P, i32, P, P,
+                                         sz, P]
+            L.tacg_expert_i8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32, i32]
+            L.tacg_expert_i8_workspace_bytes.restype = sz
             L.tacg_strerror.argtypes = [ctypes.c_int]
             L.tacg_strerror.restype = ctypes.c_char_p
             for name in ("tacg_coact_build", "tacg_reweight", "tacg_placement_load", "tacg_eval_placements",
@@ -513,16 +524,20 @@ def _score(score: str) -> int:
 def route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = "softmax", bias: Optional[torch.Tensor] = None,
           renorm: bool = False, scale: float = 1.0, balance: bool = False, want_norm: bool = False,
           ws: Optional[torch.Tensor] = None, err: Optional[torch.Tensor] = None, out: Optional[dict] = None,
-          stream=None) -> dict:
+          stream=None, groups: int = 1, top_groups: int = 1, group_best: int = 2) -> dict:
     """Top-k experts and gates of router logits [L][N][E] (tacg_route).  fam_off: None = one family of all tokens.
 
     dict(trace int16 [L][N][k], gate float32 [L][N][k], err), with want_norm or balance also norm float32 [L][N], and with
     balance D [F][L][E], tokens [F][L] (uint32 bits), balance float32 [F][L] and, for softmax scores, z float32 [F][L].
+    groups > 1 (tacg_route_grouped): the experts lie in that many groups of equal size, one after the other, and only those of the
+    top_groups groups with the largest sum of their group_best (1 or 2) largest scores (with the bias) can be chosen.
+
     Masked experts have the logit -inf; where fewer than k are left the trace holds -1 and the gate 0.  A NaN or +inf logit sets
     ERR_VALUE in err."""
     if stream is not None:  # all of the call, its buffers too, on that stream
         with torch.cuda.stream(stream):
-            return route(logits, top_k, fam_off, score, bias, renorm, scale, balance, want_norm, ws, err, out)
+            return route(logits, top_k, fam_off, score, bias, renorm, scale, balance, want_norm, ws, err, out, None, groups,
+                         top_groups, group_best)
     ptr, dtype, s_layer, s_token, (L_, N, E) = _logits(logits)
     off, F = _segments(fam_off, N)
     code = _score(score)
@@ -550,15 +565,15 @@ def route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = "softmax"
         D = tokens = b = z = None
     if err is None:
         err = _err_tensor(logits.device)
-    st = C.tacg_route(
+    st = C.tacg_route_grouped(
         ptr, dtype, s_layer, s_token, N, L_, top_k, E, off, F, code,
-        _arg(bias, "bias", torch.float32, (L_, E)), 1 if renorm else 0, float(scale),
+        _arg(bias, "bias", torch.float32, (L_, E)), 1 if renorm else 0, float(scale), groups, top_groups, group_best,
         _arg(out["trace"], "trace", torch.int16, (L_, N, top_k)), _arg(out["gate"], "gate", torch.float32, (L_, N, top_k)),
         _arg(out.get("norm"), "norm", torch.float32, (L_, N)), _arg(D, "D", torch.int32, (F, L_, E)),
         _arg(tokens, "tokens", torch.int32, (F, L_)), _arg(b, "balance", torch.float32, (F, L_)),
         _arg(z, "z", torch.float32, (F, L_)), _arg(err, "err", torch.int32, (1,)),
         _dptr(ws) if balance else None, ws.numel() if balance else 0, _stream())
-    _check("tacg_route", st)
+    _check("tacg_route" if groups == 1 else "tacg_route_grouped", st)
     out["err"] = err
     return out
 
@@ -673,4 +688,124 @@ def expert_q4(x: torch.Tensor, ids: torch.Tensor, q: torch.Tensor, scales: torch
         _arg(out, "out", x.dtype, {0: (T, k, N), 1: (T, k, N // 2), 2: (T, N)}[code]),
         _arg(err, "err", torch.int32, (1,)), _dptr(ws), ws.numel() if ws is not None else 0, _stream())
     _check("tacg_expert_q4", st)
+    return out
+
+
+def _row_tiles(N: int) -> int:
+    return -(-N // 16)
+
+
+def token_i8(x: torch.Tensor, err: Optional[torch.Tensor] = None, stream=None):
+    """Tokens [...][K] in 8 bits (tacg_token_i8): levels int8 [...][K rounded up to 64] and scale float32 [...], with
+    x ~ scale * levels.  Rows are contiguous and equally spaced.  A row with a value that is not finite gets the scale NaN and sets
+    ERR_VALUE in `err` (int32 [1], 0 at first): without one nothing reports it."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return token_i8(x, err)
+    if x.dtype not in DTYPES or not x.is_cuda or x.dim() < 1:
+        raise ValueError(f"x: expected a float device tensor [...][K], got {x.dtype} {tuple(x.shape)}")
+    lead, K = x.shape[:-1], x.shape[-1]
+    rows = x.reshape(-1, K) if x.is_contiguous() else x
+    if rows.dim() != 2 or (rows.stride(1) != 1 and K > 1):
+        raise ValueError(f"x: expected contiguous rows that are equally spaced, got strides {x.stride()}")
+    q = torch.empty(lead + (-(-K // 64) * 64,), dtype=torch.int8, device=x.device)
+    scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+    if err is None:
+        err = _err_tensor(x.device)
+    st = lib().tacg_token_i8(x.data_ptr(), DTYPES[x.dtype], rows.shape[0], K, rows.stride(0), _dptr(q), _dptr(scale),
+                             _arg(err, "err", torch.int32, (1,)), _stream())
+    _check("tacg_token_i8", st)
+    return q, scale
+
+
+def i8_pack(weight: torch.Tensor, err: Optional[torch.Tensor] = None, stream=None):
+    """Weights [H][N][K] in 8 bits with a scale for each row (tacg_i8_pack): q int8 [H][ceil(N / 16)][ceil(K / 64)][4][16][16] and
+    scale float32 [H][N].  A row with a weight that is not finite gets the scale NaN and sets ERR_VALUE in `err` (int32 [1], 0 at
+    first): without one nothing reports it."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return i8_pack(weight, err)
+    if weight.dim() != 3 or weight.dtype not in DTYPES or not weight.is_cuda or not weight.is_contiguous():
+        raise ValueError(f"weight: expected a contiguous float device tensor [H][N][K], got {weight.dtype} "
+                         f"{tuple(weight.shape)}")
+    H, N, K = weight.shape
+    dev = weight.device
+    q = torch.empty((H, _row_tiles(N), -(-K // 64), 4, 16, 16), dtype=torch.int8, device=dev)
+    scale = torch.empty((H, N), dtype=torch.float32, device=dev)
+    if err is None:
+        err = _err_tensor(dev)
+    st = lib().tacg_i8_pack(weight.data_ptr(), DTYPES[weight.dtype], H, N, K, _dptr(q), _dptr(scale),
+                            _arg(err, "err", torch.int32, (1,)), _stream())
+    _check("tacg_i8_pack", st)
+    return q, scale
+
+
+def expert_i8(x, ids: Optional[torch.Tensor], q: torch.Tensor, scale: torch.Tensor, mode: str = "each",
+              n_experts: Optional[int] = None, slot_of_expert: Optional[torch.Tensor] = None,
+              gate: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None, ws: Optional[torch.Tensor] = None,
+              err: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Products in 8-bit integers of tokens with the weights of their experts (tacg_expert_i8).
+
+    x [T][K], or [T][k][K] where every slot has its own, rows contiguous, in bfloat16, float16 or float32: rounded to 8 bits in the
+    call.  Or the pair of token_i8, for tokens that several calls take.  q, scale: the experts of this GPU (i8_pack).  ids,
+    n_experts, slot_of_expert, mode and what they leave out are those of expert_q4; ids None: shared experts, every token takes all
+    of q, slot j the j-th.  gate float32 [T][k], for "sum" (None: 1).  dtype: of the result (default: that of x or out, bfloat16
+    for a pair).  A token that is not finite gives NaN and sets ERR_VALUE in `err` (int32 [1], 0 at first; the calls of a program
+    can share one); ids out of range and bad entries of slot_of_expert set ERR_ID_RANGE and ERR_TABLE: without one nothing reports
+    them."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return expert_i8(x, ids, q, scale, mode, n_experts, slot_of_expert, gate, dtype, ws, err, out)
+    if mode not in Q4_MODES:
+        raise ValueError(f"mode: expected one of {sorted(Q4_MODES)}, got {mode!r}")
+    if q.dim() != 6 or scale.dim() != 2:
+        raise ValueError(f"q, scale: expected those of i8_pack, got {tuple(q.shape)} and {tuple(scale.shape)}")
+    (H, N), Kt = scale.shape, q.shape[2]
+    x_scale = None
+    if isinstance(x, (tuple, list)):
+        x, x_scale = x
+        if x.dtype != torch.int8:
+            raise ValueError(f"x: expected the levels and scales of token_i8, got {x.dtype}")
+        kind = I8
+    else:
+        kind = DTYPES.get(x.dtype)
+        if kind is None:
+            raise ValueError(f"x: expected bfloat16, float16 or float32, or the pair of token_i8, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError("expected a device tensor")
+    shape, stride = x.shape, x.stride()
+    T, K = (shape[0] if len(shape) else 0), shape[-1]
+    if ids is None:
+        k, E = H, H
+    else:
+        if ids.dim() != 2 or ids.dtype != torch.int16:
+            raise ValueError(f"ids: expected int16 [T][k], got {ids.dtype} {tuple(ids.shape)}")
+        T, k = ids.shape
+        E = H if n_experts is None else int(n_experts)
+    if (shape != (T, K) and shape != (T, k, K)) or -(-K // 64) != Kt or (kind == I8 and K % 64):
+        raise ValueError(f"x: expected [{T}][K] or [{T}][{k}][K] with K of the weights (up to {Kt * 64}), got {tuple(shape)}")
+    if stride[-1] != 1 and K > 1:
+        raise ValueError("x: the values of a row must be contiguous")
+    if dtype is None:
+        dtype = out.dtype if out is not None else x.dtype if kind != I8 else torch.bfloat16
+    if dtype not in DTYPES:
+        raise ValueError(f"dtype: expected bfloat16, float16 or float32, got {dtype}")
+    code = Q4_MODES[mode]
+    result = ((T, k, N), (T, k, N // 2), (T, N))[code]
+    if out is None:
+        out = torch.empty(result, dtype=dtype, device=x.device)
+    slot_stride = stride[1] if len(shape) == 3 else 0
+    C = _lib or lib()
+    need = C.tacg_expert_i8_workspace_bytes(T, k, H, N, K, code, kind, 1 if slot_stride else 0)
+    if need and (ws is None or ws.numel() < need):
+        ws = workspace(need, x.device)
+    if err is None:
+        err = _err_tensor(x.device)
+    st = C.tacg_expert_i8(
+        x.data_ptr(), kind, _arg(x_scale, "x_scale", torch.float32, shape[:-1] if slot_stride else (T,)), stride[0], slot_stride, T,
+        k, E, None if ids is None else _dptr(ids), _arg(slot_of_expert, "slot_of_expert", torch.int32, (E,)), H,
+        _arg(q, "q", torch.int8, (H, _row_tiles(N), Kt, 4, 16, 16)), _arg(scale, "scale", torch.float32, (H, N)),
+        N, K, code, _arg(gate, "gate", torch.float32, (T, k)) if code == 2 else None, _arg(out, "out", dtype, result), DTYPES[dtype],
+        _arg(err, "err", torch.int32, (1,)), _dptr(ws), ws.numel() if ws is not None else 0, _stream())
+    _check("tacg_expert_i8", st)
     return out

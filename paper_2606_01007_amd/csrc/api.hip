@@ -359,14 +359,18 @@ size_t tacg_route_workspace_bytes(int64_t n_tokens, int32_t n_layers, int32_t n_
   return tacg::route_workspace(n_tokens, n_layers, n_experts, n_fam);
 }
 
-int tacg_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
-               int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
-               int32_t score, const float* bias_or_null, int32_t renormalise, float scale, int16_t* trace, float* gate,
-               float* norm_or_null, uint32_t* D_or_null, uint32_t* tokens_or_null, float* balance_or_null,
-               float* z_or_null, uint32_t* d_err, void* workspace, size_t workspace_bytes, void* hip_stream) {
+int tacg_route_grouped(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+                       int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+                       int32_t score, const float* bias_or_null, int32_t renormalise, float scale, int32_t n_groups,
+                       int32_t top_groups, int32_t group_best, int16_t* trace, float* gate, float* norm_or_null,
+                       uint32_t* D_or_null, uint32_t* tokens_or_null, float* balance_or_null, float* z_or_null,
+                       uint32_t* d_err, void* workspace, size_t workspace_bytes, void* hip_stream) {
   const int rc = check_route(logits, dtype, stride_layer, stride_token, n_tokens, n_layers, top_k, n_experts,
                              fam_off_host, n_fam, score, renormalise, scale);
   if (rc != TACG_OK) return rc;
+  if (n_groups < 1 || top_groups < 1 || top_groups > n_groups || (group_best != 1 && group_best != 2)) return TACG_E_INVAL;
+  if (n_groups > TACG_MAX_GROUPS) return TACG_E_UNSUPPORTED;
+  if (n_experts % n_groups != 0) return TACG_E_INVAL;
   if (d_err == nullptr || (n_tokens > 0 && (trace == nullptr || gate == nullptr))) return TACG_E_INVAL;
   const bool bal = D_or_null != nullptr;
   if (bal != (tokens_or_null != nullptr) || bal != (balance_or_null != nullptr)) return TACG_E_INVAL;
@@ -376,9 +380,19 @@ int tacg_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t 
     if (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 256)) return TACG_E_INVAL;
   }
   return tacg::launch_route(logits, dtype, stride_layer, stride_token, n_tokens, n_layers, top_k, n_experts,
-                            fam_off_host, n_fam, score, bias_or_null, renormalise != 0, scale, trace, gate, norm_or_null,
-                            D_or_null, tokens_or_null, balance_or_null, z_or_null, d_err, workspace,
-                            as_stream(hip_stream));
+                            fam_off_host, n_fam, score, bias_or_null, renormalise != 0, scale, n_groups, top_groups,
+                            group_best, trace, gate, norm_or_null, D_or_null, tokens_or_null, balance_or_null, z_or_null,
+                            d_err, workspace, as_stream(hip_stream));
+}
+
+int tacg_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
+               int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
+               int32_t score, const float* bias_or_null, int32_t renormalise, float scale, int16_t* trace, float* gate,
+               float* norm_or_null, uint32_t* D_or_null, uint32_t* tokens_or_null, float* balance_or_null,
+               float* z_or_null, uint32_t* d_err, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return tacg_route_grouped(logits, dtype, stride_layer, stride_token, n_tokens, n_layers, top_k, n_experts, fam_off_host,
+                            n_fam, score, bias_or_null, renormalise, scale, 1, 1, 1, trace, gate, norm_or_null, D_or_null,
+                            tokens_or_null, balance_or_null, z_or_null, d_err, workspace, workspace_bytes, hip_stream);
 }
 
 int tacg_route_backward(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
@@ -448,6 +462,64 @@ int tacg_expert_q4(const void* x, int32_t dtype, int64_t stride_token, int64_t s
   return tacg::launch_expert_q4(x, dtype, stride_token, stride_slot, n_tokens, top_k, n_experts, ids,
                                 slot_of_expert_or_null, n_held, q, scales, zeros_or_null, group, n_rows, n_cols, mode,
                                 gate_or_null, out, d_err, workspace, as_stream(hip_stream));
+}
+
+static bool is_float(int32_t dtype) { return dtype == TACG_F32 || is_half(dtype); }
+
+int tacg_token_i8(const void* x, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride, int8_t* q, float* scale,
+                  uint32_t* d_err, void* hip_stream) {
+  if (!is_float(dtype) || n_rows < 0 || n_cols < 1 || row_stride < 0 || d_err == nullptr) return TACG_E_INVAL;
+  if (n_cols > TACG_MAX_WIDTH || n_rows >= (int64_t(1) << 31)) return TACG_E_UNSUPPORTED;
+  if (n_rows == 0) return TACG_OK;
+  if (x == nullptr || !aligned(x, dtype == TACG_F32 ? 4 : 2) || q == nullptr || !aligned(q, 16)) return TACG_E_INVAL;
+  if (scale == nullptr || !aligned(scale, 4)) return TACG_E_INVAL;
+  return tacg::launch_token_i8(x, dtype, row_stride, 0, n_rows, 1, n_cols, q, scale, d_err, as_stream(hip_stream));
+}
+
+int tacg_i8_pack(const void* w, int32_t dtype, int32_t n_matrices, int32_t n_rows, int32_t n_cols, int8_t* q, float* scale,
+                 uint32_t* d_err, void* hip_stream) {
+  if (!is_float(dtype) || n_matrices < 0 || n_rows < 1 || n_cols < 1 || d_err == nullptr) return TACG_E_INVAL;
+  if (n_matrices > TACG_MAX_EXPERTS || n_rows > TACG_MAX_WIDTH || n_cols > TACG_MAX_WIDTH) return TACG_E_UNSUPPORTED;
+  if (n_matrices == 0) return TACG_OK;
+  if (w == nullptr || !aligned(w, dtype == TACG_F32 ? 4 : 2) || q == nullptr || !aligned(q, 16)) return TACG_E_INVAL;
+  if (scale == nullptr || !aligned(scale, 4)) return TACG_E_INVAL;
+  return tacg::launch_i8_pack(w, dtype, n_matrices, n_rows, n_cols, q, scale, d_err, as_stream(hip_stream));
+}
+
+size_t tacg_expert_i8_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode,
+                                      int32_t dtype, int32_t per_slot) {
+  if (n_tokens < 0 || top_k < 1 || n_held < 0 || n_rows < 1 || n_cols < 1) return 0;
+  return tacg::expert_i8_workspace(n_tokens, top_k, n_cols, dtype, per_slot != 0);
+}
+
+int tacg_expert_i8(const void* x, int32_t dtype, const float* x_scale_or_null, int64_t stride_token, int64_t stride_slot,
+                   int64_t n_tokens, int32_t top_k, int32_t n_experts, const int16_t* ids_or_null,
+                   const int32_t* slot_of_expert_or_null, int32_t n_held, const int8_t* w, const float* w_scale, int32_t n_rows,
+                   int32_t n_cols, int32_t mode, const float* gate_or_null, void* out, int32_t out_dtype, uint32_t* d_err,
+                   void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const bool shared = ids_or_null == nullptr && n_tokens != 0, levels = dtype == TACG_I8;
+  if (n_held < 0) return TACG_E_INVAL;
+  const int rc = check_trace(nullptr, 0, 1, top_k, shared ? n_held : n_experts, kNoTokens, 1);
+  if (rc != TACG_OK) return rc;
+  if (shared && (top_k != n_held || slot_of_expert_or_null != nullptr)) return TACG_E_INVAL;
+  if ((!levels && !is_float(dtype)) || !is_float(out_dtype) || n_tokens < 0 || n_rows < 1 || n_cols < 1 || d_err == nullptr)
+    return TACG_E_INVAL;
+  if (stride_token < 0 || stride_slot < 0 || levels != (x_scale_or_null != nullptr)) return TACG_E_INVAL;
+  if (mode != TACG_Q4_EACH && mode != TACG_Q4_GLU && mode != TACG_Q4_SUM) return TACG_E_INVAL;
+  if (mode == TACG_Q4_GLU && n_rows % 2 != 0) return TACG_E_INVAL;
+  if (n_rows > TACG_MAX_WIDTH || n_cols > TACG_MAX_WIDTH || n_held > TACG_MAX_EXPERTS) return TACG_E_UNSUPPORTED;
+  if (n_tokens >= (int64_t(1) << 27) / top_k) return TACG_E_UNSUPPORTED;
+  if (n_held > 0 && (w == nullptr || w_scale == nullptr || !aligned(w, 16) || !aligned(w_scale, 4))) return TACG_E_INVAL;
+  if (n_tokens == 0) return TACG_OK;
+  if (x == nullptr || !aligned(x, levels ? 16 : dtype == TACG_F32 ? 4 : 2)) return TACG_E_INVAL;
+  if (levels && (stride_token % 16 != 0 || stride_slot % 16 != 0 || !aligned(x_scale_or_null, 4))) return TACG_E_INVAL;
+  if (out == nullptr || !aligned(out, out_dtype == TACG_F32 ? 4 : 2)) return TACG_E_INVAL;
+  const size_t need =
+      tacg_expert_i8_workspace_bytes(n_tokens, top_k, n_held, n_rows, n_cols, mode, dtype, stride_slot > 0);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 256))) return TACG_E_INVAL;
+  return tacg::launch_expert_i8(x, dtype, x_scale_or_null, stride_token, stride_slot, n_tokens, top_k, n_experts, ids_or_null,
+                                slot_of_expert_or_null, n_held, w, w_scale, n_rows, n_cols, mode, gate_or_null, out, out_dtype,
+                                d_err, workspace, as_stream(hip_stream));
 }
 
 const char* tacg_strerror(int status) {

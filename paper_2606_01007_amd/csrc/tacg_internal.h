@@ -109,8 +109,8 @@ int launch_jain(const uint32_t* load, int32_t n_place, int32_t n_layers, int32_t
 size_t route_workspace(int64_t n_tokens, int32_t n_layers, int32_t n_experts, int32_t n_fam);
 int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,
                  int32_t n_layers, int32_t top_k, int32_t n_experts, const int64_t* fam_off_host, int32_t n_fam,
-                 int32_t score, const float* bias, bool renorm, float scale, int16_t* trace, float* gate, float* norm,
-                 uint32_t* D, uint32_t* tokens, float* balance, float* z, uint32_t* d_err, void* workspace,
+                 int32_t score, const float* bias, bool renorm, float scale, int32_t n_groups, int32_t top_groups,
+                 int32_t group_best, int16_t* trace, float* gate, float* norm, uint32_t* D, uint32_t* tokens, float* balance, float* z, uint32_t* d_err, void* workspace,
                  hipStream_t stream);
 int launch_route_backward(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token,
                           int64_t n_tokens, int32_t n_layers, int32_t top_k, int32_t n_experts,
@@ -129,5 +129,16 @@ int launch_expert_q4(const void* x, int32_t dtype, int64_t x_stride_token, int64
                      int32_t n_held, const uint8_t* q, const void* scales, const uint8_t* zeros, int32_t group,
                      int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate, void* out, uint32_t* d_err,
                      void* workspace, hipStream_t stream);
+
+// ---- products in 8-bit integers ---------------------------------------------------------------
+int launch_i8_pack(const void* w, int32_t dtype, int64_t n_matrices, int32_t n_rows, int32_t n_cols, int8_t* q, float* scale,
+                   uint32_t* d_err, hipStream_t stream);
+int launch_token_i8(const void* x, int32_t dtype, int64_t stride_token, int64_t stride_slot, int64_t n_rows, int32_t rows_of_token,
+                    int32_t n_cols, int8_t* q, float* scale, uint32_t* d_err, hipStream_t stream);
+size_t expert_i8_workspace(int64_t n_tokens, int32_t top_k, int32_t n_cols, int32_t dtype, bool slots);
+int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
+                     int32_t top_k, int32_t n_experts, const int16_t* ids, const int32_t* slot_of_expert, int32_t n_held,
+                     const int8_t* w, const float* w_scale, int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate,
+                     void* out, int32_t out_dtype, uint32_t* d_err, void* workspace, hipStream_t stream);
 
 }  // namespace tacg

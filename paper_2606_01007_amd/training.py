@@ -19,8 +19,9 @@ from . import _fam_off, route, route_backward
 
 class _Route(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, logits, top_k, fam_off, score, bias, renorm, scale, kept):
-        r = route(logits, top_k, fam_off, score=score, bias=bias, renorm=renorm, scale=scale, balance=True)
+    def forward(ctx, logits, top_k, fam_off, score, bias, renorm, scale, groups, kept):
+        r = route(logits, top_k, fam_off, score=score, bias=bias, renorm=renorm, scale=scale, balance=True, groups=groups[0],
+                  top_groups=groups[1], group_best=groups[2])
         kept.update(r)
         ctx.save_for_backward(logits, r["trace"], r["norm"], r["D"], r["tokens"])
         ctx.how = (fam_off, score, renorm, scale)
@@ -37,15 +38,16 @@ class _Route(torch.autograd.Function):
         grad = route_backward(logits, trace, norm, fam_off, D=D, tokens=tokens, grad_gate=whole(grad_gate),
                               grad_balance=whole(grad_balance), grad_z=whole(grad_z) if score == "softmax" else None,
                               score=score, renorm=renorm, scale=scale)
-        return grad, None, None, None, None, None, None, None
+        return grad, None, None, None, None, None, None, None, None
 
 
 def balanced_route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = "softmax",
-                   bias: Optional[torch.Tensor] = None, renorm: bool = False, scale: float = 1.0):
+                   bias: Optional[torch.Tensor] = None, renorm: bool = False, scale: float = 1.0, groups: int = 1,
+                   top_groups: int = 1, group_best: int = 2):
     """(gate [L][N][k], balance [F][L], z [F][L], the dict of `route`): gate, balance and z are differentiable with respect to the
-    logits.  z is 0 for sigmoid scores, which have none."""
+    logits.  z is 0 for sigmoid scores, which have none.  groups, top_groups and group_best limit the selection as in `route`."""
     kept: dict = {}
     if fam_off is not None:
         fam_off = _fam_off(fam_off).tolist()  # a copy: the backward pass takes the same families, whatever becomes of the caller's
-    gate, balance, z = _Route.apply(logits, top_k, fam_off, score, bias, renorm, scale, kept)
+    gate, balance, z = _Route.apply(logits, top_k, fam_off, score, bias, renorm, scale, (groups, top_groups, group_best), kept)
     return gate, balance, z, kept

@@ -473,7 +473,7 @@ int tacg_token_i8(const void* x, int32_t dtype, int64_t n_rows, int32_t n_cols, 
   if (n_rows == 0) return TACG_OK;
   if (x == nullptr || !aligned(x, dtype == TACG_F32 ? 4 : 2) || q == nullptr || !aligned(q, 16)) return TACG_E_INVAL;
   if (scale == nullptr || !aligned(scale, 4)) return TACG_E_INVAL;
-  return tacg::launch_token_i8(x, dtype, row_stride, 0, n_rows, 1, n_cols, q, scale, d_err, as_stream(hip_stream));
+  return tacg::launch_token_i8(x, dtype, row_stride, n_rows, n_cols, q, scale, d_err, as_stream(hip_stream));
 }
 
 int tacg_i8_pack(const void* w, int32_t dtype, int32_t n_matrices, int32_t n_rows, int32_t n_cols, int8_t* q, float* scale,
@@ -489,7 +489,7 @@ int tacg_i8_pack(const void* w, int32_t dtype, int32_t n_matrices, int32_t n_row
 size_t tacg_expert_i8_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode,
                                       int32_t dtype, int32_t per_slot) {
   if (n_tokens < 0 || top_k < 1 || n_held < 0 || n_rows < 1 || n_cols < 1) return 0;
-  return tacg::expert_i8_workspace(n_tokens, top_k, n_cols, dtype, per_slot != 0);
+  return tacg::expert_i8_workspace(n_tokens, top_k, n_held, n_rows, n_cols, mode, dtype, per_slot != 0);
 }
 
 int tacg_expert_i8(const void* x, int32_t dtype, const float* x_scale_or_null, int64_t stride_token, int64_t stride_slot,

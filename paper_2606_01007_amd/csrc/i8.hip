@@ -9,6 +9,7 @@
 // i8_product: a lane per weight row, a workgroup per (token, slot), or summed per token.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "tacg_internal.h"
 
@@ -28,6 +29,7 @@ struct I8Args {
   const int8_t* w;
   const float* w_scale;
   const float* gate;        // [T][k] or null: 1
+  float* part;              // [T][k][N]: the products of the pairs that are summed later, or null
   void* out;
   uint32_t* err;
 };
@@ -75,6 +77,39 @@ struct Rounder {
   }
 };
 
+// A lane's values of a row: pieces of eight, 64 lanes after another.
+constexpr int kChunk = 8, kWaveChunk = 64 * kChunk;
+
+template <int DTYPE>
+__device__ __forceinline__ void load_chunk(const void* x, int64_t first, int c, int K, float (&v)[kChunk]) {
+  using T = std::conditional_t<DTYPE == TACG_F32, float, std::conditional_t<DTYPE == TACG_BF16, __bf16, _Float16>>;
+  const T* p = static_cast<const T*>(x) + first + c;
+  if (c + kChunk <= K) {
+    T piece[kChunk];
+    __builtin_memcpy(piece, p, sizeof(piece));  // rows need not start at multiples of 16 bytes
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) v[i] = static_cast<float>(piece[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) v[i] = c + i < K ? static_cast<float>(p[i]) : 0.0f;
+  }
+}
+__device__ __forceinline__ uint32_t largest(const float (&v)[kChunk], uint32_t m) {
+#pragma unroll
+  for (int i = 0; i < kChunk; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  return m;
+}
+__device__ __forceinline__ uint2 levels_of(const Rounder& level, const float (&v)[kChunk], bool bad) {
+  uint32_t o[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t lo = __builtin_amdgcn_perm(level(v[4 * h + 1]), level(v[4 * h]), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(level(v[4 * h + 3]), level(v[4 * h + 2]), 0x04000c0cu);
+    o[h] = bad ? 0u : lo | hi;
+  }
+  return make_uint2(o[0], o[1]);
+}
+
 struct TokenArgs {
   const void* x;
   int64_t stride_token, stride_slot, rows;
@@ -84,28 +119,43 @@ struct TokenArgs {
   uint32_t* err;
 };
 
-// grid: rows.
-template <int DTYPE>
-__global__ __launch_bounds__(256) void i8_tokens(TokenArgs a) {
-  __shared__ uint32_t most[4];
-  const int tid = threadIdx.x;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const int64_t first = r / a.k * a.stride_token + r % a.k * a.stride_slot;
-    uint32_t m = 0;  // magnitudes order as their bits, and what is not finite is above all others
-    for (int c = tid; c < a.K; c += 256) m = max(m, __float_as_uint(load<DTYPE>(a.x, first + c)) & 0x7fffffffu);
-    for (int o = 32; o >= 1; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o, 64)));
-    if ((tid & 63) == 0) most[tid >> 6] = m;
-    __syncthreads();
-    m = max(max(most[0], most[1]), max(most[2], most[3]));
-    const bool bad = m >= 0x7f800000u;
-    const Rounder level(bad ? 0.0f : __uint_as_float(m));
-    for (int c = tid; c < a.Kp; c += 256)
-      a.q[r * a.Kp + c] = c < a.K && !bad ? static_cast<int8_t>(level(load<DTYPE>(a.x, first + c)) & 0xffu) : int8_t(0);
-    if (tid == 0) {
-      a.scale[r] = bad ? NAN : __uint_as_float(m) / 127.0f;
-      if (bad) atomicOr(a.err, TACG_ERR_VALUE);
+// One row by one wave.  CH: pieces of a lane that stay in registers; 0: the row is read twice.
+template <int DTYPE, int CH>
+__device__ __forceinline__ void round_row(const TokenArgs& a, int64_t r, int lane) {
+  const int64_t first = a.k == 1 ? r * a.stride_token : r / a.k * a.stride_token + r % a.k * a.stride_slot;
+  uint32_t m = 0;  // magnitudes order as their bits, and what is not finite is above all others
+  float v[CH ? CH : 1][kChunk];
+  if constexpr (CH > 0) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load_chunk<DTYPE>(a.x, first, c * kWaveChunk + lane * kChunk, a.K, v[c]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) m = largest(v[c], m);
+  } else {
+    for (int c = lane * kChunk; c < a.K; c += kWaveChunk) {
+      load_chunk<DTYPE>(a.x, first, c, a.K, v[0]);
+      m = largest(v[0], m);
     }
-    __syncthreads();
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o, 64)));
+  const bool bad = m >= 0x7f800000u;
+  const Rounder level(bad ? 0.0f : __uint_as_float(m));
+  int8_t* q = a.q + r * a.Kp;
+  if constexpr (CH > 0) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int at = c * kWaveChunk + lane * kChunk;
+      if (at < a.Kp) *reinterpret_cast<uint2*>(q + at) = levels_of(level, v[c], bad);
+    }
+  } else {
+    for (int at = lane * kChunk; at < a.Kp; at += kWaveChunk) {
+      load_chunk<DTYPE>(a.x, first, at, a.K, v[0]);
+      *reinterpret_cast<uint2*>(q + at) = levels_of(level, v[0], bad);
+    }
+  }
+  if (lane == 0) {
+    a.scale[r] = bad ? NAN : __uint_as_float(m) / 127.0f;
+    if (bad) atomicOr(a.err, TACG_ERR_VALUE);
   }
 }
 
@@ -146,56 +196,399 @@ __global__ __launch_bounds__(256) void i8_pack_kernel(PackArgs a) {
   }
 }
 
-__device__ __forceinline__ const int4* row_of(const I8Args& a, int h, int n) {
-  return reinterpret_cast<const int4*>(a.w + (static_cast<int64_t>(h) * a.row_tiles + n / kTileRows) * a.col_tiles * kTileBytes) +
-         n % kTileRows;
-}
 
-// A weight row's sum with a token's levels.
-__device__ __forceinline__ int dot(const I8Args& a, int h, int n, const int8_t* levels) {
-  const int4* w = row_of(a, h, n);
-  const int4* x = reinterpret_cast<const int4*>(levels);
-  int s = 0;
-  for (int p = 0; p < a.col_tiles * (kTileCols / kPiece); ++p) {
-    const int4 u = w[static_cast<int64_t>(p) * kTileRows], v = x[p];
-    s = __builtin_amdgcn_sdot4(u.x, v.x, s, false);
-    s = __builtin_amdgcn_sdot4(u.y, v.y, s, false);
-    s = __builtin_amdgcn_sdot4(u.z, v.z, s, false);
-    s = __builtin_amdgcn_sdot4(u.w, v.w, s, false);
+// ---- the order of the pairs -------------------------------------------------------------------
+
+// Pairs by their matrix: order[first[h] .. first[h + 1]) are those of matrix h, order[first[H] ..) those that are served elsewhere.  The
+// tiles of `tile` pairs of matrix h have the numbers first[h] / tile + h and following: no two matrices share one, and no matrix
+// needs to know the others' tiles.  tiles[i] = matrix and first pair of tile i, or -1.
+struct Plan {
+  int32_t* order;
+  int32_t* first;     // [H + 2]
+  int2* tiles;
+  int32_t tile, n_tiles;
+};
+
+constexpr int kScan = 8;  // pairs of a lane at a time
+
+// One workgroup per matrix (and one for what is served elsewhere) looks through all pairs, twice: no workgroup waits for another.
+__device__ void plan_block(const I8Args& a, const Plan& p, int h) {
+  __shared__ int16_t place[TACG_MAX_EXPERTS];
+  __shared__ int lower, equal, cursor;
+  const int tid = threadIdx.x;
+  const int pairs = static_cast<int>(a.n_tokens * a.k);
+  if (tid == 0) lower = equal = cursor = 0;
+  for (int e = tid; e < a.E; e += 256) {
+    const int v = a.slot != nullptr ? a.slot[e] : e;
+    place[e] = static_cast<int16_t>(v < 0 ? -1 : v < a.H ? v : kBadTable);
   }
-  return s;
-}
-
-// grid: (blocks of 256 output columns, pairs or, summed, tokens).
-__global__ __launch_bounds__(256) void i8_product(I8Args a) {
-  const bool sum = a.mode == TACG_Q4_SUM, glu = a.mode == TACG_Q4_GLU;
-  const int width = glu ? a.N / 2 : a.N, n = blockIdx.x * 256 + threadIdx.x;
-  const int64_t units = sum ? a.n_tokens : a.n_tokens * a.k;
-  for (int64_t u = blockIdx.y; u < units; u += gridDim.y) {
-    float y = 0.0f;
-    for (int i = 0; i < (sum ? a.k : 1); ++i) {
-      const int64_t t = sum ? u : u / a.k;
-      const int j = sum ? i : static_cast<int>(u % a.k);
-      const int64_t pair = t * a.k + j;
-      const int h = place_of(a, pair, j);
-      if (h < 0) {
-        if (h < -1 && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.err, h == kBadId ? TACG_ERR_ID_RANGE : TACG_ERR_TABLE);
-        continue;
+  __syncthreads();
+  uint32_t bad = 0;
+  auto scan = [&](auto use) {
+    for (int base = tid * kScan; base < pairs; base += 256 * kScan) {
+      int16_t id[kScan];
+      const int n = min(kScan, pairs - base);
+      if (n == kScan) __builtin_memcpy(id, a.ids + base, sizeof(id));
+      else
+        for (int i = 0; i < kScan; ++i) id[i] = i < n ? a.ids[base + i] : int16_t(-1);
+      int at[kScan];
+#pragma unroll
+      for (int i = 0; i < kScan; ++i) {
+        const bool in = static_cast<uint32_t>(static_cast<int>(id[i])) < static_cast<uint32_t>(a.E);
+        at[i] = in ? place[in ? id[i] : 0] : id[i] == -1 ? -1 : kBadId;
       }
-      if (n >= width) continue;
-      const int8_t* levels = a.x + t * a.x_token + j * a.x_slot;
-      const float sx = a.x_scale[a.slots ? pair : t];
-      const float* sw = a.w_scale + static_cast<int64_t>(h) * a.N;
-      float v = static_cast<float>(dot(a, h, n, levels)) * (sx * sw[n]);
-      if (glu) {
-        const float up = static_cast<float>(dot(a, h, n + width, levels)) * (sx * sw[n + width]);
-        v = v / (1.0f + __expf(-v)) * up;
-      }
-      if (sum) y += (a.gate != nullptr ? a.gate[pair] : 1.0f) * v;
-      else y = v;
+      use(base, n, at);
     }
-    if (n < width) store(a.out, u * width + n, y, a.out_dtype);
+  };
+  int below = 0, own = 0;
+  scan([&](int, int n, const int (&at)[kScan]) {
+#pragma unroll
+    for (int i = 0; i < kScan; ++i) {
+      if (i >= n) continue;
+      bad |= at[i] == kBadId ? TACG_ERR_ID_RANGE : at[i] == kBadTable ? TACG_ERR_TABLE : 0u;
+      below += at[i] >= 0 && at[i] < h;
+      own += at[i] == h || (h == a.H && at[i] < 0);
+    }
+  });
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) below += __shfl_xor(below, o, 64);
+  int all = own;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) all += __shfl_xor(all, o, 64);
+  if ((tid & 63) == 0) {
+    atomicAdd(&lower, below);
+    atomicAdd(&equal, all);
   }
+  if (h == 0 && bad != 0) atomicOr(a.err, bad);
+  barrier_after_lds_atomics();
+  const int from = lower, count = equal;
+  if (count > 0) {
+    int at = own > 0 ? from + atomicAdd(&cursor, own) : 0;  // their order within a matrix does not matter to any result
+    scan([&](int base, int n, const int (&v)[kScan]) {
+#pragma unroll
+      for (int i = 0; i < kScan; ++i)
+        if (i < n && (v[i] == h || (h == a.H && v[i] < 0))) p.order[at++] = base + i;
+    });
+  }
+  const int begin = from / p.tile + h;
+  const int end = h < a.H ? (from + count) / p.tile + h + 1 : p.n_tiles;
+  for (int i = begin + tid; i < end; i += 256) {
+    const int start = from + (i - begin) * p.tile;
+    p.tiles[i] = h < a.H && start < from + count ? make_int2(h, start) : make_int2(-1, 0);
+  }
+  if (tid == 0) {
+    p.first[h] = from;
+    if (h == a.H) p.first[h + 1] = from + count;
+  }
+}
+
+// grid: n_plan workgroups for the order of the pairs, then workgroups of four waves, a row of tokens each.
+template <int DTYPE, int CH>
+__global__ __launch_bounds__(256) void i8_prepare(TokenArgs t, I8Args a, Plan p, int n_plan, bool skip) {
+  if (static_cast<int>(blockIdx.x) < n_plan) {
+    plan_block(a, p, blockIdx.x);
+    return;
+  }
+  const int lane = threadIdx.x & 63;
+  const int64_t step = static_cast<int64_t>(gridDim.x - n_plan) * 4;
+  for (int64_t r = static_cast<int64_t>(blockIdx.x - n_plan) * 4 + (threadIdx.x >> 6); r < t.rows; r += step)
+    if (!skip || place_of(a, r, 0) >= 0) round_row<DTYPE, CH>(t, r, lane);
+}
+
+// ---- products ----------------------------------------------------------------------------------
+
+typedef __attribute__((ext_vector_type(4))) int int4v;
+
+constexpr int kWaves = 4, kRowFrags = 4;
+constexpr int kWaveRows = kRowFrags * kTileRows;  // weight rows of a wave; gated: half of them of each kind
+
+// What a lane does of its part of a tile's results: 4 consecutive rows of a token.
+__device__ __forceinline__ void put(const I8Args& a, int64_t row, int n, int width, const float (&y)[4], void* out, int dtype) {
+  const int64_t at = row * width + n;
+  if (n + 4 <= width && width % 4 == 0) {
+    if (dtype == TACG_F32) {
+      float4 v = make_float4(y[0], y[1], y[2], y[3]);
+      __builtin_memcpy(static_cast<float*>(out) + at, &v, 16);
+    } else if (dtype == TACG_BF16) {
+      __bf16 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = static_cast<__bf16>(y[i]);
+      __builtin_memcpy(static_cast<__bf16*>(out) + at, v, 8);
+    } else {
+      _Float16 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = static_cast<_Float16>(y[i]);
+      __builtin_memcpy(static_cast<_Float16*>(out) + at, v, 8);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < width) store(out, at + i, y[i], dtype);
+  }
+}
+
+struct Unit {
+  int h, first, count;  // matrix, its tile's first pair in the order and number of pairs
+  int n0;               // first output column
+};
+
+__device__ __forceinline__ int64_t pair_of(const I8Args& a, const Plan& p, const Unit& u, int i) {
+  return a.ids == nullptr ? static_cast<int64_t>(u.first + i) * a.k + u.h : p.order[u.first + i];
+}
+
+// JT: blocks of 16 tokens.
+template <int JT>
+__device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, const Unit& u, char* lds) {
+  constexpr int kLoads = (JT * 2 + kWaves - 1) / kWaves;  // fragments of tokens that a wave brings in a step
+  constexpr int kStage = JT * 2 * 1024;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool glu = a.mode == TACG_Q4_GLU;
+  const int width = glu ? a.N / 2 : a.N;
+  const int n0 = u.n0 + wave * (glu ? kWaveRows / 2 : kWaveRows);
+  // where the lane's pieces of the weights lie
+  const char* w = reinterpret_cast<const char*>(a.w) + static_cast<int64_t>(u.h) * a.row_tiles * a.col_tiles * kTileBytes;
+  uint32_t at[kRowFrags];
+#pragma unroll
+  for (int i = 0; i < kRowFrags; ++i) {
+    int row = glu ? n0 + (i / 2) * kTileRows : n0 + i * kTileRows;
+    row = min(row, width - 1) + (lane & 15);
+    row = glu && (i & 1) ? min(row + width, a.row_tiles * kTileRows - 1) : min(row, a.row_tiles * kTileRows - 1);
+    at[i] = static_cast<uint32_t>(row / kTileRows) * a.col_tiles * kTileBytes + (lane >> 4) * 256 + row % kTileRows * kPiece;
+  }
+  const int8_t* token[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int f = wave + i * kWaves;
+    const int64_t pair = pair_of(a, p, u, min((f >> 1) * 16 + (lane & 15), u.count - 1));
+    token[i] = a.x + pair / a.k * a.x_token + pair % a.k * a.x_slot + (lane >> 4) * kPiece;
+  }
+  int4v acc[kRowFrags][JT];
+#pragma unroll
+  for (int i = 0; i < kRowFrags; ++i)
+#pragma unroll
+    for (int j = 0; j < JT; ++j) acc[i][j] = int4v{0, 0, 0, 0};
+  const int last = a.col_tiles - 1, steps = (a.col_tiles + 1) / 2;
+  auto load_weights = [&](int s, int4v (&v)[2][kRowFrags]) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      const uint32_t c = static_cast<uint32_t>(min(2 * s + kk, last)) * kTileBytes;
+#pragma unroll
+      for (int i = 0; i < kRowFrags; ++i) v[kk][i] = *reinterpret_cast<const int4v*>(w + (at[i] + c));
+    }
+  };
+  auto load_tokens = [&](int s, int4v (&v)[kLoads]) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int f = wave + i * kWaves, c = 2 * s + (f & 1);
+      v[i] = int4v{0, 0, 0, 0};  // past the last column: nothing, whatever the weights are
+      if (c <= last && (JT * 2 % kWaves == 0 || f < JT * 2)) v[i] = *reinterpret_cast<const int4v*>(token[i] + c * kTileCols);
+    }
+  };
+  auto keep_tokens = [&](char* to, const int4v (&v)[kLoads]) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int f = wave + i * kWaves;
+      if (JT * 2 % kWaves == 0 || f < JT * 2) *reinterpret_cast<int4v*>(to + f * 1024 + lane * 16) = v[i];
+    }
+  };
+  int4v wa[2][kRowFrags], wb[2][kRowFrags], tk[kLoads];
+  load_tokens(0, tk);
+  load_weights(0, wa);
+  keep_tokens(lds, tk);
+  auto step = [&](int s, int4v (&now)[2][kRowFrags], int4v (&next)[2][kRowFrags]) {
+    __syncthreads();
+    const int ahead = min(s + 1, steps - 1);
+    load_tokens(ahead, tk);
+    load_weights(ahead, next);
+    __builtin_amdgcn_sched_barrier(0);
+    const char* from = lds + (s & 1) * kStage;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int j = 0; j < JT; ++j) {
+        const int4v t = *reinterpret_cast<const int4v*>(from + (2 * j + kk) * 1024 + lane * 16);
+#pragma unroll
+        for (int i = 0; i < kRowFrags; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[kk][i], t, acc[i][j], 0, 0, 0);
+      }
+    keep_tokens(lds + ((s + 1) & 1) * kStage, tk);
+  };
+  for (int s = 0; s < steps; s += 2) {
+    step(s, wa, wb);
+    if (s + 1 < steps) step(s + 1, wb, wa);
+  }
+  // results
+  const float* sw = a.w_scale + static_cast<int64_t>(u.h) * a.N;
+  const bool sum = a.mode == TACG_Q4_SUM;
+#pragma unroll
+  for (int j = 0; j < JT; ++j) {
+    const int i0 = j * 16 + (lane & 15);
+    if (i0 >= u.count) continue;
+    const int64_t pair = pair_of(a, p, u, i0);
+    const float sx = a.x_scale[a.slots ? pair : pair / a.k];
+#pragma unroll
+    for (int i = 0; i < (glu ? kRowFrags / 2 : kRowFrags); ++i) {
+      const int n = n0 + i * kTileRows + (lane >> 4) * 4;
+      if (n >= width) continue;
+      float y[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = min(n + r, width - 1);
+        if (glu) {
+          const float g = static_cast<float>(acc[2 * i & 3][j][r]) * (sx * sw[row]);
+          const float v = static_cast<float>(acc[(2 * i + 1) & 3][j][r]) * (sx * sw[row + width]);
+          y[r] = g / (1.0f + __expf(-g)) * v;
+        } else {
+          y[r] = static_cast<float>(acc[i][j][r]) * (sx * sw[row]);
+        }
+      }
+      if (sum && a.part != nullptr) put(a, pair, n, width, y, a.part, TACG_F32);
+      else {
+        if (sum && a.gate != nullptr)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[r] *= a.gate[pair];
+        put(a, pair, n, width, y, a.out, a.out_dtype);
+      }
+    }
+  }
+}
+
+// What is served elsewhere is 0.
+__device__ __forceinline__ void clear_block(const I8Args& a, const Plan& p, int block, int blocks) {
+  const int width = a.mode == TACG_Q4_GLU ? a.N / 2 : a.N, size = a.out_dtype == TACG_F32 ? 4 : 2;
+  const int64_t bytes = static_cast<int64_t>(width) * size;
+  for (int i = p.first[a.H] + block; i < p.first[a.H + 1]; i += blocks) {
+    char* row = static_cast<char*>(a.out) + p.order[i] * bytes;
+    const int64_t head = min(bytes, static_cast<int64_t>(-reinterpret_cast<uintptr_t>(row) & 15)), body = (bytes - head) / 16;
+    if (threadIdx.x < head / 2) reinterpret_cast<int16_t*>(row)[threadIdx.x] = 0;
+    for (int64_t c = threadIdx.x; c < body; c += 256) reinterpret_cast<int4*>(row + head)[c] = make_int4(0, 0, 0, 0);
+    const int64_t done = head + body * 16;
+    if (threadIdx.x < (bytes - done) / 2) reinterpret_cast<int16_t*>(row + done)[threadIdx.x] = 0;
+  }
+}
+
+// grid: tiles of pairs x blocks of output columns, then `clear` workgroups.
+template <int TILE>
+__global__ __launch_bounds__(256, 2) void i8_tiles(I8Args a, Plan p, int blocks, int clear) {
+  __shared__ alignas(16) char lds[2 * (TILE / 16) * 2 * 1024];
+  const int total = p.n_tiles * blocks;
+  int w = blockIdx.x;
+  if (w >= total) {
+    clear_block(a, p, w - total, clear);
+    return;
+  }
+  // neighbouring units share tokens or weights: each of the eight dies takes a run of them, as workgroups go to the dies in turn
+  const int share = total / 8;
+  if (w < share * 8) w = (w & 7) * share + (w >> 3);
+  const int tile = w / blocks;
+  Unit u;
+  u.n0 = (w - tile * blocks) * kWaves * (a.mode == TACG_Q4_GLU ? kWaveRows / 2 : kWaveRows);
+  if (a.ids == nullptr) {
+    const int per = (static_cast<int>(a.n_tokens) + TILE - 1) / TILE;
+    u.h = tile / per;
+    u.first = (tile - u.h * per) * TILE;
+    u.count = static_cast<int>(a.n_tokens) - u.first;
+  } else {
+    const int2 t = p.tiles[tile];
+    u.h = t.x;
+    u.first = t.y;
+    if (u.h < 0) return;
+    u.count = p.first[u.h + 1] - u.first;
+  }
+  u.count = min(u.count, TILE);
+  const int jt = (u.count + 15) / 16;
+  if constexpr (TILE >= 128) {
+    if (jt > 6) return tile_product<8>(a, p, u, lds);
+    if (jt > 4) return tile_product<6>(a, p, u, lds);
+    if (jt > 2) return tile_product<4>(a, p, u, lds);
+  }
+  if (jt > 1) return tile_product<2>(a, p, u, lds);
+  tile_product<1>(a, p, u, lds);
+}
+
+// Sums over the slots of a token, in order.  grid: (blocks of 1024 output columns, tokens).
+__global__ __launch_bounds__(256) void i8_combine(I8Args a) {
+  const int n = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (n >= a.N) return;
+  for (int64_t t = blockIdx.y; t < a.n_tokens; t += gridDim.y) {
+    float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < a.k; ++j) {
+      const int64_t pair = t * a.k + j;
+      if (place_of(a, pair, j) < 0) continue;
+      const float g = a.gate != nullptr ? a.gate[pair] : 1.0f;
+      const float* v = a.part + pair * a.N + n;
+      float f[4];
+      if (a.N % 4 == 0) __builtin_memcpy(f, v, 16);
+      else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = n + i < a.N ? v[i] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] += g * f[i];
+    }
+    put(a, t, n, a.N, y, a.out, a.out_dtype);
+  }
+}
+
+template <int DTYPE>
+void start_prepare(const TokenArgs& t, const I8Args& a, const Plan& p, int n_plan, bool skip, hipStream_t stream) {
+  const dim3 grid(static_cast<uint32_t>(n_plan + std::min<int64_t>((t.rows + 3) / 4, 1 << 20)));
+  if (t.K <= kWaveChunk) i8_prepare<DTYPE, 1><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
+  else if (t.K <= 2 * kWaveChunk) i8_prepare<DTYPE, 2><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
+  else if (t.K <= 4 * kWaveChunk) i8_prepare<DTYPE, 4><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
+  else if (t.K <= 8 * kWaveChunk) i8_prepare<DTYPE, 8><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
+  else i8_prepare<DTYPE, 0><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
+}
+
+void start_prepare(const TokenArgs& t, int32_t dtype, const I8Args& a, const Plan& p, int n_plan, bool skip, hipStream_t stream) {
+  if (dtype == TACG_F32) start_prepare<TACG_F32>(t, a, p, n_plan, skip, stream);
+  else if (dtype == TACG_BF16) start_prepare<TACG_BF16>(t, a, p, n_plan, skip, stream);
+  else start_prepare<TACG_F16>(t, a, p, n_plan, skip, stream);
+}
+
+TokenArgs token_args(const void* x, int64_t stride_token, int64_t stride_slot, int64_t n_rows, int32_t rows_of_token, int32_t n_cols,
+                     int8_t* q, float* scale, uint32_t* d_err) {
+  TokenArgs t{};
+  t.x = x;
+  t.stride_token = stride_token;
+  t.stride_slot = stride_slot;
+  t.rows = n_rows;
+  t.k = rows_of_token;
+  t.K = n_cols;
+  t.Kp = (n_cols + kTileCols - 1) / kTileCols * kTileCols;
+  t.q = q;
+  t.scale = scale;
+  t.err = d_err;
+  return t;
+}
+
+// Pairs of a tile: as many as there are weight rows to share them with, unless few pairs fall to a matrix.
+int tile_of(int64_t pairs, int32_t n_held) { return pairs > 24 * static_cast<int64_t>(n_held) ? 128 : 32; }
+
+// The parts of a call's workspace.
+struct Space {
+  int8_t* levels;
+  float* scales;
+  float* part;
+  Plan plan;
+  size_t bytes;
+};
+
+Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
+               bool slots) {
+  Space s{};
+  Carver ws{static_cast<char*>(base), 0};
+  const int64_t pairs = n_tokens * top_k, rows = slots ? pairs : n_tokens;
+  if (dtype != TACG_I8) {
+    s.levels = ws.take<int8_t>(rows * ((n_cols + kTileCols - 1) / kTileCols * kTileCols));
+    s.scales = ws.take<float>(rows);
+  }
+  s.plan.tile = tile_of(pairs, n_held);
+  s.plan.n_tiles = static_cast<int32_t>(pairs / s.plan.tile + n_held);
+  s.plan.order = ws.take<int32_t>(pairs);
+  s.plan.first = ws.take<int32_t>(n_held + 2);
+  s.plan.tiles = ws.take<int2>(s.plan.n_tiles);
+  if (mode == TACG_Q4_SUM && top_k > 1) s.part = ws.take<float>(pairs * n_rows);
+  s.bytes = ws.used;
+  return s;
 }
 
 }  // namespace
@@ -219,38 +612,24 @@ int launch_i8_pack(const void* w, int32_t dtype, int64_t n_matrices, int32_t n_r
   return hipGetLastError() == hipSuccess ? TACG_OK : TACG_E_DEVICE;
 }
 
-int launch_token_i8(const void* x, int32_t dtype, int64_t stride_token, int64_t stride_slot, int64_t n_rows, int32_t rows_of_token,
-                    int32_t n_cols, int8_t* q, float* scale, uint32_t* d_err, hipStream_t stream) {
-  TokenArgs a{};
-  a.x = x;
-  a.stride_token = stride_token;
-  a.stride_slot = stride_slot;
-  a.rows = n_rows;
-  a.k = rows_of_token;
-  a.K = n_cols;
-  a.Kp = (n_cols + kTileCols - 1) / kTileCols * kTileCols;
-  a.q = q;
-  a.scale = scale;
-  a.err = d_err;
-  const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(n_rows, 1 << 20)));
-  if (dtype == TACG_F32) i8_tokens<TACG_F32><<<grid, 256, 0, stream>>>(a);
-  else if (dtype == TACG_BF16) i8_tokens<TACG_BF16><<<grid, 256, 0, stream>>>(a);
-  else i8_tokens<TACG_F16><<<grid, 256, 0, stream>>>(a);
+int launch_token_i8(const void* x, int32_t dtype, int64_t row_stride, int64_t n_rows, int32_t n_cols, int8_t* q, float* scale,
+                    uint32_t* d_err, hipStream_t stream) {
+  start_prepare(token_args(x, row_stride, 0, n_rows, 1, n_cols, q, scale, d_err), dtype, I8Args{}, Plan{}, 0, false, stream);
   return hipGetLastError() == hipSuccess ? TACG_OK : TACG_E_DEVICE;
 }
 
-size_t expert_i8_workspace(int64_t n_tokens, int32_t top_k, int32_t n_cols, int32_t dtype, bool slots) {
-  if (dtype == TACG_I8) return 0;
-  const size_t rows = static_cast<size_t>(n_tokens) * (slots ? top_k : 1);
-  return align256(rows * ((n_cols + kTileCols - 1) / kTileCols * kTileCols)) + align256(rows * sizeof(float));
+size_t expert_i8_workspace(int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
+                           bool slots) {
+  return space_of(nullptr, n_tokens, top_k, n_held, n_rows, n_cols, mode, dtype, slots).bytes;
 }
 
 int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
                      int32_t top_k, int32_t n_experts, const int16_t* ids, const int32_t* slot_of_expert, int32_t n_held,
                      const int8_t* w, const float* w_scale, int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate,
                      void* out, int32_t out_dtype, uint32_t* d_err, void* workspace, hipStream_t stream) {
-  I8Args a{};
   const bool slots = stride_slot != 0;
+  Space s = space_of(workspace, n_tokens, top_k, n_held, n_rows, n_cols, mode, dtype, slots);
+  I8Args a{};
   a.n_tokens = n_tokens;
   a.k = top_k;
   a.E = n_experts;
@@ -266,29 +645,41 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
   a.w = w;
   a.w_scale = w_scale;
   a.gate = gate;
+  a.part = s.part;
   a.out = out;
   a.err = d_err;
+  const int width = mode == TACG_Q4_GLU ? n_rows / 2 : n_rows, per = kWaves * (mode == TACG_Q4_GLU ? kWaveRows / 2 : kWaveRows);
+  const int blocks = (width + per - 1) / per;
+  if (ids == nullptr) s.plan.n_tiles = static_cast<int>((n_tokens + s.plan.tile - 1) / s.plan.tile) * n_held;
+  const int clear = ids != nullptr && s.part == nullptr ? static_cast<int>(std::min<int64_t>(n_tokens * top_k, 256)) : 0;
+  const int64_t grid = static_cast<int64_t>(s.plan.n_tiles) * blocks + clear;
+  if (grid >= (int64_t(1) << 32) / 256) return TACG_E_UNSUPPORTED;  // threads that a launch holds; results of more than 288 GB
+  const int n_plan = ids != nullptr ? n_held + 1 : 0;
   if (dtype == TACG_I8) {
     a.x = static_cast<const int8_t*>(x);
     a.x_scale = x_scale;
     a.x_token = stride_token;
     a.x_slot = stride_slot;
+    if (n_plan > 0) start_prepare(TokenArgs{}, TACG_BF16, a, s.plan, n_plan, false, stream);
   } else {
-    Carver ws{static_cast<char*>(workspace), 0};
-    const int64_t rows = n_tokens * (slots ? top_k : 1), width = static_cast<int64_t>(a.col_tiles) * kTileCols;
-    int8_t* q = ws.take<int8_t>(rows * width);
-    float* scale = ws.take<float>(rows);
-    const int rc = launch_token_i8(x, dtype, stride_token, stride_slot, rows, slots ? top_k : 1, n_cols, q, scale, d_err, stream);
-    if (rc != TACG_OK) return rc;
-    a.x = q;
-    a.x_scale = scale;
+    const int64_t width = static_cast<int64_t>(a.col_tiles) * kTileCols;
+    const int64_t rows = n_tokens * (slots ? top_k : 1);
+    const TokenArgs t = token_args(x, stride_token, stride_slot, rows, slots ? top_k : 1, n_cols, s.levels, s.scales, d_err);
+    a.x = s.levels;
+    a.x_scale = s.scales;
     a.x_token = width * (slots ? top_k : 1);
     a.x_slot = slots ? width : 0;
+    start_prepare(t, dtype, a, s.plan, n_plan, slots && ids != nullptr, stream);
   }
-  const int64_t units = mode == TACG_Q4_SUM ? n_tokens : n_tokens * top_k;
-  const int width = mode == TACG_Q4_GLU ? n_rows / 2 : n_rows;
-  const dim3 grid((width + 255) / 256, static_cast<uint32_t>(std::min<int64_t>(units, 65535)));
-  i8_product<<<grid, 256, 0, stream>>>(a);
+  if (hipGetLastError() != hipSuccess) return TACG_E_DEVICE;
+  if (grid > 0) {
+    if (s.plan.tile == 128) i8_tiles<128><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(a, s.plan, blocks, clear);
+    else i8_tiles<32><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(a, s.plan, blocks, clear);
+  }
+  if (s.part != nullptr) {
+    const dim3 sums((n_rows + 1023) / 1024, static_cast<uint32_t>(std::min<int64_t>(n_tokens, 65535)));
+    i8_combine<<<sums, 256, 0, stream>>>(a);
+  }
   return hipGetLastError() == hipSuccess ? TACG_OK : TACG_E_DEVICE;
 }
 

@@ -450,9 +450,9 @@ int tacg_expert_i8(const void* x, int32_t dtype, const float* x_scale_or_null, i
                    int32_t n_cols, int32_t mode, const float* gate_or_null, void* out, int32_t out_dtype, uint32_t* d_err,
                    void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* per_slot: whether stride_slot > 0 */
-size_t tacg_expert_i8_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode,
-                                      int32_t dtype, int32_t per_slot);
+/* n_experts: n_held where ids is NULL; per_slot: whether stride_slot > 0 */
+size_t tacg_expert_i8_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows,
+                                      int32_t n_cols, int32_t mode, int32_t dtype, int32_t per_slot);
 
 /* Human-readable text of a status code (static storage). */
 const char* tacg_strerror(int status);

@@ -110,7 +110,7 @@ def lib():
             L.tacg_i8_pack.argtypes = [P, i32, i32, i32, i32, P, P, P, P]
             L.tacg_expert_i8.argtypes = [P, i32, P, i64, i64, i64, i32, i32, P, P, i32, P, P, i32, i32, i32, P, P, i32, P, P,
                                          sz, P]
-            L.tacg_expert_i8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32, i32]
+            L.tacg_expert_i8_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32, i32, i32]
             L.tacg_expert_i8_workspace_bytes.restype = sz
             L.tacg_strerror.argtypes = [ctypes.c_int]
             L.tacg_strerror.restype = ctypes.c_char_p
@@ -796,7 +796,7 @@ def expert_i8(x, ids: Optional[torch.Tensor], q: torch.Tensor, scale: torch.Tens
         out = torch.empty(result, dtype=dtype, device=x.device)
     slot_stride = stride[1] if len(shape) == 3 else 0
     C = _lib or lib()
-    need = C.tacg_expert_i8_workspace_bytes(T, k, H, N, K, code, kind, 1 if slot_stride else 0)
+    need = C.tacg_expert_i8_workspace_bytes(T, k, E, H, N, K, code, kind, 1 if slot_stride else 0)
     if need and (ws is None or ws.numel() < need):
         ws = workspace(need, x.device)
     if err is None:

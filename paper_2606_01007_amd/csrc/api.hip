@@ -486,10 +486,10 @@ int tacg_i8_pack(const void* w, int32_t dtype, int32_t n_matrices, int32_t n_row
   return tacg::launch_i8_pack(w, dtype, n_matrices, n_rows, n_cols, q, scale, d_err, as_stream(hip_stream));
 }
 
-size_t tacg_expert_i8_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode,
-                                      int32_t dtype, int32_t per_slot) {
-  if (n_tokens < 0 || top_k < 1 || n_held < 0 || n_rows < 1 || n_cols < 1) return 0;
-  return tacg::expert_i8_workspace(n_tokens, top_k, n_held, n_rows, n_cols, mode, dtype, per_slot != 0);
+size_t tacg_expert_i8_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows,
+                                      int32_t n_cols, int32_t mode, int32_t dtype, int32_t per_slot) {
+  if (n_tokens < 0 || top_k < 1 || n_experts < 0 || n_held < 0 || n_rows < 1 || n_cols < 1) return 0;
+  return tacg::expert_i8_workspace(n_tokens, top_k, n_experts, n_held, n_rows, n_cols, mode, dtype, per_slot != 0);
 }
 
 int tacg_expert_i8(const void* x, int32_t dtype, const float* x_scale_or_null, int64_t stride_token, int64_t stride_slot,
@@ -515,7 +515,7 @@ int tacg_expert_i8(const void* x, int32_t dtype, const float* x_scale_or_null, i
   if (levels && (stride_token % 16 != 0 || stride_slot % 16 != 0 || !aligned(x_scale_or_null, 4))) return TACG_E_INVAL;
   if (out == nullptr || !aligned(out, out_dtype == TACG_F32 ? 4 : 2)) return TACG_E_INVAL;
   const size_t need =
-      tacg_expert_i8_workspace_bytes(n_tokens, top_k, n_held, n_rows, n_cols, mode, dtype, stride_slot > 0);
+      tacg_expert_i8_workspace_bytes(n_tokens, top_k, shared ? n_held : n_experts, n_held, n_rows, n_cols, mode, dtype, stride_slot > 0);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned(workspace, 256))) return TACG_E_INVAL;
   return tacg::launch_expert_i8(x, dtype, x_scale_or_null, stride_token, stride_slot, n_tokens, top_k, n_experts, ids_or_null,
                                 slot_of_expert_or_null, n_held, w, w_scale, n_rows, n_cols, mode, gate_or_null, out, out_dtype,

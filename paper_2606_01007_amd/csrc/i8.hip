@@ -16,6 +16,8 @@
 namespace tacg {
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) int int4v;
+
 constexpr int kTileRows = 16, kTileCols = 64, kTileBytes = kTileRows * kTileCols, kPiece = 16;
 
 struct I8Args {
@@ -209,66 +211,82 @@ struct Plan {
   int32_t tile, n_tiles;
 };
 
-constexpr int kScan = 8;  // pairs of a lane at a time
+constexpr int kScan = 8, kBatch = 4, kSegment = 8;  // pairs of a load, loads of a batch, batches whose pairs are remembered
+constexpr int kBatchPairs = 256 * kScan * kBatch, kSegmentPairs = kBatchPairs * kSegment;
 
-// One workgroup per matrix (and one for what is served elsewhere) looks through all pairs, twice: no workgroup waits for another.
+// One workgroup per matrix (and one for what is served elsewhere) looks through all pairs: none waits for another, and no launch is
+// needed to add up counts.  Up to 65536 pairs are read once, with a bit in LDS for each; more are read twice.
 __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
-  __shared__ int16_t place[TACG_MAX_EXPERTS];
+  __shared__ int place[TACG_MAX_EXPERTS];
   __shared__ int lower, equal, cursor;
+  __shared__ uint32_t own[kSegment][256];  // a lane reads what it wrote itself
   const int tid = threadIdx.x;
   const int pairs = static_cast<int>(a.n_tokens * a.k);
   if (tid == 0) lower = equal = cursor = 0;
-  for (int e = tid; e < a.E; e += 256) {
-    const int v = a.slot != nullptr ? a.slot[e] : e;
-    place[e] = static_cast<int16_t>(v < 0 ? -1 : v < a.H ? v : kBadTable);
+  if (tid < a.E) {
+    const int v = a.slot != nullptr ? a.slot[tid] : tid;
+    place[tid] = v < 0 ? -1 : v < a.H ? v : kBadTable;
   }
   __syncthreads();
   uint32_t bad = 0;
-  auto scan = [&](auto use) {
-    for (int base = tid * kScan; base < pairs; base += 256 * kScan) {
-      int16_t id[kScan];
-      const int n = min(kScan, pairs - base);
-      if (n == kScan) __builtin_memcpy(id, a.ids + base, sizeof(id));
-      else
-        for (int i = 0; i < kScan; ++i) id[i] = i < n ? a.ids[base + i] : int16_t(-1);
-      int at[kScan];
+  int below = 0;
+  // the lane's pairs of a batch: base + i * 2048 + tid * 8 and the seven behind it, a bit each
+  auto batch = [&](int base) {
+    int4v id[kBatch];  // eight ids each
 #pragma unroll
-      for (int i = 0; i < kScan; ++i) {
-        const bool in = static_cast<uint32_t>(static_cast<int>(id[i])) < static_cast<uint32_t>(a.E);
-        at[i] = in ? place[in ? id[i] : 0] : id[i] == -1 ? -1 : kBadId;
+    for (int i = 0; i < kBatch; ++i) {
+      const int at = base + (i * 256 + tid) * kScan;
+      id[i] = int4v{-1, -1, -1, -1};
+      if (at + kScan <= pairs) __builtin_memcpy(&id[i], a.ids + at, 16);
+      else if (at < pairs)
+#pragma unroll
+        for (int e = 0; e < kScan; ++e)
+          if (at + e < pairs) id[i][e / 2] = e % 2 ? (id[i][e / 2] & 0xffff) | (a.ids[at + e] << 16) : (id[i][e / 2] & ~0xffff) | (a.ids[at + e] & 0xffff);
+    }
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int at = base + (i * 256 + tid) * kScan;
+#pragma unroll
+      for (int e = 0; e < kScan; ++e) {
+        const int id16 = e % 2 ? id[i][e / 2] >> 16 : static_cast<int16_t>(id[i][e / 2]);
+        const bool in = static_cast<uint32_t>(id16) < static_cast<uint32_t>(a.E);
+        int v = place[in ? id16 : 0];
+        if (!in) v = id16 == -1 ? -1 : kBadId;
+        bad |= v == kBadId ? TACG_ERR_ID_RANGE : v == kBadTable ? TACG_ERR_TABLE : 0u;
+        below += v >= 0 && v < h;
+        const bool is = at + e < pairs && (h < a.H ? v == h : v < 0);
+        mine |= static_cast<uint32_t>(is) << (i * kScan + e);
       }
-      use(base, n, at);
     }
+    return mine;
   };
-  int below = 0, own = 0;
-  scan([&](int, int n, const int (&at)[kScan]) {
+  int count = 0;
+  for (int base = 0; base < pairs; base += kBatchPairs) {
+    const uint32_t m = batch(base);
+    own[base / kBatchPairs % kSegment][tid] = m;
+    count += __popc(m);
+  }
+  const int mine = count;
 #pragma unroll
-    for (int i = 0; i < kScan; ++i) {
-      if (i >= n) continue;
-      bad |= at[i] == kBadId ? TACG_ERR_ID_RANGE : at[i] == kBadTable ? TACG_ERR_TABLE : 0u;
-      below += at[i] >= 0 && at[i] < h;
-      own += at[i] == h || (h == a.H && at[i] < 0);
-    }
-  });
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) below += __shfl_xor(below, o, 64);
-  int all = own;
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) all += __shfl_xor(all, o, 64);
+  for (int o = 32; o >= 1; o >>= 1) {
+    below += __shfl_xor(below, o, 64);
+    count += __shfl_xor(count, o, 64);
+  }
   if ((tid & 63) == 0) {
     atomicAdd(&lower, below);
-    atomicAdd(&equal, all);
+    atomicAdd(&equal, count);
   }
   if (h == 0 && bad != 0) atomicOr(a.err, bad);
   barrier_after_lds_atomics();
-  const int from = lower, count = equal;
-  if (count > 0) {
-    int at = own > 0 ? from + atomicAdd(&cursor, own) : 0;  // their order within a matrix does not matter to any result
-    scan([&](int base, int n, const int (&v)[kScan]) {
-#pragma unroll
-      for (int i = 0; i < kScan; ++i)
-        if (i < n && (v[i] == h || (h == a.H && v[i] < 0))) p.order[at++] = base + i;
-    });
+  const int from = lower;
+  count = equal;
+  int at = from + (mine > 0 ? atomicAdd(&cursor, mine) : 0);  // the order of a matrix' pairs does not matter to any result
+  for (int base = 0; base < pairs && count > 0; base += kBatchPairs) {
+    for (uint32_t m = pairs > kSegmentPairs ? batch(base) : own[base / kBatchPairs][tid]; m != 0; m &= m - 1) {
+      const int bit = __ffs(m) - 1;
+      p.order[at++] = base + (bit / kScan * 256 + tid) * kScan + bit % kScan;
+    }
   }
   const int begin = from / p.tile + h;
   const int end = h < a.H ? (from + count) / p.tile + h + 1 : p.n_tiles;
@@ -297,10 +315,9 @@ __global__ __launch_bounds__(256) void i8_prepare(TokenArgs t, I8Args a, Plan p,
 
 // ---- products ----------------------------------------------------------------------------------
 
-typedef __attribute__((ext_vector_type(4))) int int4v;
+constexpr int kManyTile = 128, kFewTile = 32;  // pairs of a tile
 
-constexpr int kWaves = 4, kRowFrags = 4;
-constexpr int kWaveRows = kRowFrags * kTileRows;  // weight rows of a wave; gated: half of them of each kind
+constexpr int kWaves = 4;
 
 // What a lane does of its part of a tile's results: 4 consecutive rows of a token.
 __device__ __forceinline__ void put(const I8Args& a, int64_t row, int n, int width, const float (&y)[4], void* out, int dtype) {
@@ -336,120 +353,222 @@ __device__ __forceinline__ int64_t pair_of(const I8Args& a, const Plan& p, const
   return a.ids == nullptr ? static_cast<int64_t>(u.first + i) * a.k + u.h : p.order[u.first + i];
 }
 
-// JT: blocks of 16 tokens.
-template <int JT>
-__device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, const Unit& u, char* lds) {
-  constexpr int kLoads = (JT * 2 + kWaves - 1) / kWaves;  // fragments of tokens that a wave brings in a step
-  constexpr int kStage = JT * 2 * 1024;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const bool glu = a.mode == TACG_Q4_GLU;
-  const int width = glu ? a.N / 2 : a.N;
-  const int n0 = u.n0 + wave * (glu ? kWaveRows / 2 : kWaveRows);
-  // where the lane's pieces of the weights lie
-  const char* w = reinterpret_cast<const char*>(a.w) + static_cast<int64_t>(u.h) * a.row_tiles * a.col_tiles * kTileBytes;
-  uint32_t at[kRowFrags];
+// Where a lane's piece of a block of 16 weight rows lies in its matrix: its row's 16 bytes of the tile's first 64 columns.  Gated: RF / 2
+// blocks of gate rows and the same rows of the other kind after each.
+template <int RF>
+__device__ __forceinline__ void weight_rows(const I8Args& a, int n0, bool glu, int width, uint32_t (&at)[RF]) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int i = 0; i < kRowFrags; ++i) {
-    int row = glu ? n0 + (i / 2) * kTileRows : n0 + i * kTileRows;
-    row = min(row, width - 1) + (lane & 15);
-    row = glu && (i & 1) ? min(row + width, a.row_tiles * kTileRows - 1) : min(row, a.row_tiles * kTileRows - 1);
+  for (int i = 0; i < RF; ++i) {
+    int row = min(n0 + (glu ? i / 2 : i) * kTileRows, width - 1) + (lane & 15) + (glu && (i & 1) ? width : 0);
+    row = min(row, a.row_tiles * kTileRows - 1);
     at[i] = static_cast<uint32_t>(row / kTileRows) * a.col_tiles * kTileBytes + (lane >> 4) * 256 + row % kTileRows * kPiece;
   }
-  const int8_t* token[kLoads];
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int f = wave + i * kWaves;
-    const int64_t pair = pair_of(a, p, u, min((f >> 1) * 16 + (lane & 15), u.count - 1));
-    token[i] = a.x + pair / a.k * a.x_token + pair % a.k * a.x_slot + (lane >> 4) * kPiece;
-  }
-  int4v acc[kRowFrags][JT];
-#pragma unroll
-  for (int i = 0; i < kRowFrags; ++i)
-#pragma unroll
-    for (int j = 0; j < JT; ++j) acc[i][j] = int4v{0, 0, 0, 0};
-  const int last = a.col_tiles - 1, steps = (a.col_tiles + 1) / 2;
-  auto load_weights = [&](int s, int4v (&v)[2][kRowFrags]) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      const uint32_t c = static_cast<uint32_t>(min(2 * s + kk, last)) * kTileBytes;
-#pragma unroll
-      for (int i = 0; i < kRowFrags; ++i) v[kk][i] = *reinterpret_cast<const int4v*>(w + (at[i] + c));
-    }
-  };
-  auto load_tokens = [&](int s, int4v (&v)[kLoads]) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int f = wave + i * kWaves, c = 2 * s + (f & 1);
-      v[i] = int4v{0, 0, 0, 0};  // past the last column: nothing, whatever the weights are
-      if (c <= last && (JT * 2 % kWaves == 0 || f < JT * 2)) v[i] = *reinterpret_cast<const int4v*>(token[i] + c * kTileCols);
-    }
-  };
-  auto keep_tokens = [&](char* to, const int4v (&v)[kLoads]) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int f = wave + i * kWaves;
-      if (JT * 2 % kWaves == 0 || f < JT * 2) *reinterpret_cast<int4v*>(to + f * 1024 + lane * 16) = v[i];
-    }
-  };
-  int4v wa[2][kRowFrags], wb[2][kRowFrags], tk[kLoads];
-  load_tokens(0, tk);
-  load_weights(0, wa);
-  keep_tokens(lds, tk);
-  auto step = [&](int s, int4v (&now)[2][kRowFrags], int4v (&next)[2][kRowFrags]) {
-    __syncthreads();
-    const int ahead = min(s + 1, steps - 1);
-    load_tokens(ahead, tk);
-    load_weights(ahead, next);
-    __builtin_amdgcn_sched_barrier(0);
-    const char* from = lds + (s & 1) * kStage;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int j = 0; j < JT; ++j) {
-        const int4v t = *reinterpret_cast<const int4v*>(from + (2 * j + kk) * 1024 + lane * 16);
-#pragma unroll
-        for (int i = 0; i < kRowFrags; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[kk][i], t, acc[i][j], 0, 0, 0);
-      }
-    keep_tokens(lds + ((s + 1) & 1) * kStage, tk);
-  };
-  for (int s = 0; s < steps; s += 2) {
-    step(s, wa, wb);
-    if (s + 1 < steps) step(s + 1, wb, wa);
-  }
-  // results
+}
+
+__device__ __forceinline__ const char* matrix_of(const I8Args& a, int h) {
+  return reinterpret_cast<const char*>(a.w) + static_cast<int64_t>(h) * a.row_tiles * a.col_tiles * kTileBytes;
+}
+__device__ __forceinline__ const int8_t* token_of(const I8Args& a, int64_t pair) {
+  return a.x + pair / a.k * a.x_token + pair % a.k * a.x_slot + ((threadIdx.x & 63) >> 4) * kPiece;
+}
+__device__ __forceinline__ int4v load16(const void* p) { return *static_cast<const int4v*>(p); }
+
+// Results of a wave: lane n + 16 q holds rows 4 q .. 4 q + 3 of a block for token n.
+template <int RF, int JT>
+__device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Unit& u, int n0, const int4v (&acc)[RF][JT]) {
+  const int lane = threadIdx.x & 63;
+  const bool glu = a.mode == TACG_Q4_GLU, sum = a.mode == TACG_Q4_SUM;
+  const int width = glu ? a.N / 2 : a.N;
   const float* sw = a.w_scale + static_cast<int64_t>(u.h) * a.N;
-  const bool sum = a.mode == TACG_Q4_SUM;
 #pragma unroll
   for (int j = 0; j < JT; ++j) {
     const int i0 = j * 16 + (lane & 15);
     if (i0 >= u.count) continue;
     const int64_t pair = pair_of(a, p, u, i0);
     const float sx = a.x_scale[a.slots ? pair : pair / a.k];
+    const float gate = sum && a.part == nullptr && a.gate != nullptr ? a.gate[pair] : 1.0f;
+    auto scaled = [&](int sum32, int row) { return static_cast<float>(sum32) * (sx * sw[row]); };
+    if (glu) {
+      if constexpr (RF > 1) {
 #pragma unroll
-    for (int i = 0; i < (glu ? kRowFrags / 2 : kRowFrags); ++i) {
+        for (int i = 0; i < RF / 2; ++i) {
+          const int n = n0 + i * kTileRows + (lane >> 4) * 4;
+          if (n >= width) continue;
+          float y[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int row = min(n + r, width - 1);
+            const float g = scaled(acc[2 * i][j][r], row);
+            y[r] = g / (1.0f + __expf(-g)) * scaled(acc[2 * i + 1][j][r], row + width);
+          }
+          put(a, pair, n, width, y, a.out, a.out_dtype);
+        }
+      }
+      continue;
+    }
+#pragma unroll
+    for (int i = 0; i < RF; ++i) {
       const int n = n0 + i * kTileRows + (lane >> 4) * 4;
       if (n >= width) continue;
       float y[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = min(n + r, width - 1);
-        if (glu) {
-          const float g = static_cast<float>(acc[2 * i & 3][j][r]) * (sx * sw[row]);
-          const float v = static_cast<float>(acc[(2 * i + 1) & 3][j][r]) * (sx * sw[row + width]);
-          y[r] = g / (1.0f + __expf(-g)) * v;
-        } else {
-          y[r] = static_cast<float>(acc[i][j][r]) * (sx * sw[row]);
-        }
-      }
+      for (int r = 0; r < 4; ++r) y[r] = scaled(acc[i][j][r], min(n + r, width - 1)) * gate;
       if (sum && a.part != nullptr) put(a, pair, n, width, y, a.part, TACG_F32);
-      else {
-        if (sum && a.gate != nullptr)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) y[r] *= a.gate[pair];
-        put(a, pair, n, width, y, a.out, a.out_dtype);
-      }
+      else put(a, pair, n, width, y, a.out, a.out_dtype);
     }
   }
+}
+
+// Many tokens: a wave has 64 weight rows and all tokens of the tile, JT blocks of 16.  Steps of 64 columns: weights go from memory to the
+// registers of the wave that needs them, two steps ahead; tokens through LDS, one step ahead, and from there two blocks ahead.
+template <int JT>
+__device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, const Unit& u, char* lds) {
+  constexpr int RF = 4, kLoads = (JT + kWaves - 1) / kWaves;  // blocks of tokens that a wave brings in a step
+  constexpr int kStage = JT * 1024;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool glu = a.mode == TACG_Q4_GLU;
+  const int width = glu ? a.N / 2 : a.N;
+  const int n0 = u.n0 + wave * (glu ? RF / 2 : RF) * kTileRows;
+  const char* w = matrix_of(a, u.h);
+  uint32_t at[RF];
+  weight_rows<RF>(a, n0, glu, width, at);
+  const int8_t* token[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) token[i] = token_of(a, pair_of(a, p, u, min((wave + i * kWaves) * 16 + (lane & 15), u.count - 1)));
+  int4v acc[RF][JT];
+#pragma unroll
+  for (int i = 0; i < RF; ++i)
+#pragma unroll
+    for (int j = 0; j < JT; ++j) acc[i][j] = int4v{0, 0, 0, 0};
+  const int last = a.col_tiles - 1;
+  auto load_weights = [&](int c, int4v (&v)[RF]) {
+    const uint32_t from = static_cast<uint32_t>(min(c, last)) * kTileBytes;
+#pragma unroll
+    for (int i = 0; i < RF; ++i) v[i] = load16(w + (at[i] + from));
+  };
+  int4v tk[kLoads];
+  auto load_tokens = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) tk[i] = load16(token[i] + min(c, last) * kTileCols);
+  };
+  auto keep_tokens = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int j = wave + i * kWaves;
+      if (JT % kWaves == 0 || j < JT) *reinterpret_cast<int4v*>(lds + (c & 1) * kStage + j * 1024 + lane * 16) = tk[i];
+    }
+  };
+  int4v w0[RF], w1[RF], w2[RF];
+  load_tokens(0);
+  load_weights(0, w0);
+  load_weights(1, w1);
+  keep_tokens(0);
+  auto step = [&](int c, int4v (&now)[RF], int4v (&far)[RF]) {
+    __syncthreads();
+    load_tokens(c + 1);
+    load_weights(c + 2, far);
+    const char* from = lds + (c & 1) * kStage + lane * 16;
+    int4v t[2];
+    t[0] = load16(from);
+    if (JT > 1) t[1] = load16(from + 1024);
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < RF; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[i], t[j & 1], acc[i][j], 0, 0, 0);
+      if (j + 2 < JT) t[j & 1] = load16(from + (j + 2) * 1024);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    keep_tokens(c + 1);
+  };
+  for (int c = 0;; c += 3) {
+    step(c, w0, w2);
+    if (c + 1 > last) break;
+    step(c + 1, w1, w0);
+    if (c + 2 > last) break;
+    step(c + 2, w2, w1);
+    if (c + 3 > last) break;
+  }
+  finish<RF, JT>(a, p, u, n0, acc);
+}
+
+// Few tokens: the time is that of the weights' loads.  A wave has RF blocks of 16 weight rows; weights and tokens go straight to its
+// registers, DEPTH steps of 64 columns ahead, without a barrier.  SPLIT: the four waves have the same rows and a quarter of the
+// columns each, and add their (exact) sums up in LDS.
+template <int RF, int JT, bool SPLIT>
+__device__ __forceinline__ void stream_product(const I8Args& a, const Plan& p, const Unit& u, int4v* lds) {
+  constexpr int DEPTH = 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool glu = a.mode == TACG_Q4_GLU;
+  const int width = glu ? a.N / 2 : a.N;
+  const int n0 = u.n0 + (SPLIT ? 0 : wave * (glu ? RF / 2 : RF) * kTileRows);
+  const char* w = matrix_of(a, u.h);
+  uint32_t at[RF];
+  weight_rows<RF>(a, n0, glu, width, at);
+  const int8_t* token[JT];
+#pragma unroll
+  for (int j = 0; j < JT; ++j) token[j] = token_of(a, pair_of(a, p, u, min(j * 16 + (lane & 15), u.count - 1)));
+  int4v acc[RF][JT];
+#pragma unroll
+  for (int i = 0; i < RF; ++i)
+#pragma unroll
+    for (int j = 0; j < JT; ++j) acc[i][j] = int4v{0, 0, 0, 0};
+  const int begin = SPLIT ? a.col_tiles * wave / kWaves : 0, end = SPLIT ? a.col_tiles * (wave + 1) / kWaves : a.col_tiles;
+  int4v v[DEPTH][RF], t[DEPTH][JT];
+  auto load = [&](int c, int d) {
+    const uint32_t from = static_cast<uint32_t>(c) * kTileBytes;
+#pragma unroll
+    for (int i = 0; i < RF; ++i) v[d][i] = load16(w + (at[i] + from));
+#pragma unroll
+    for (int j = 0; j < JT; ++j) t[d][j] = load16(token[j] + c * kTileCols);
+  };
+  auto multiply = [&](int d) {
+#pragma unroll
+    for (int j = 0; j < JT; ++j)
+#pragma unroll
+      for (int i = 0; i < RF; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[d][i], t[d][j], acc[i][j], 0, 0, 0);
+  };
+  const int last = max(end - 1, 0);
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) load(min(begin + d, last), d);
+  int c = begin;
+  for (; c + 2 * DEPTH <= end; c += DEPTH) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      multiply(d);
+      load(c + d + DEPTH, d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // the last ones: DEPTH or more, unless there are fewer in all
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (c + d < end) {
+      multiply(d);
+      if (c + d + DEPTH < end) load(c + d + DEPTH, d);
+    }
+  c += DEPTH;
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (c + d < end) multiply(d);
+  if constexpr (SPLIT) {
+    if (wave > 0) {
+#pragma unroll
+      for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int j = 0; j < JT; ++j) lds[((wave - 1) * RF * JT + i * JT + j) * 64 + lane] = acc[i][j];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int o = 0; o < kWaves - 1; ++o)
+#pragma unroll
+      for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int j = 0; j < JT; ++j) acc[i][j] += lds[(o * RF * JT + i * JT + j) * 64 + lane];
+  }
+  finish<RF, JT>(a, p, u, n0, acc);
 }
 
 // What is served elsewhere is 0.
@@ -466,22 +585,22 @@ __device__ __forceinline__ void clear_block(const I8Args& a, const Plan& p, int 
   }
 }
 
-// grid: tiles of pairs x blocks of output columns, then `clear` workgroups.
+// The unit of a workgroup: a tile of pairs and a block of `rows` output columns.  Neighbouring units share tokens or weights: each
+// of the eight dies takes a run of them, as workgroups go to the dies in turn.
 template <int TILE>
-__global__ __launch_bounds__(256, 2) void i8_tiles(I8Args a, Plan p, int blocks, int clear) {
-  __shared__ alignas(16) char lds[2 * (TILE / 16) * 2 * 1024];
-  const int total = p.n_tiles * blocks;
+__device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int blocks, int rows, int clear, Unit& u) {
+  // tiles that there are: those of pairs served here
+  const int total = (a.ids == nullptr ? p.n_tiles : __builtin_amdgcn_readfirstlane(p.first[a.H]) / TILE + a.H) * blocks;
   int w = blockIdx.x;
   if (w >= total) {
-    clear_block(a, p, w - total, clear);
-    return;
+    const int all = p.n_tiles * blocks;
+    if (w >= all) clear_block(a, p, w - all, clear);
+    return false;
   }
-  // neighbouring units share tokens or weights: each of the eight dies takes a run of them, as workgroups go to the dies in turn
   const int share = total / 8;
   if (w < share * 8) w = (w & 7) * share + (w >> 3);
   const int tile = w / blocks;
-  Unit u;
-  u.n0 = (w - tile * blocks) * kWaves * (a.mode == TACG_Q4_GLU ? kWaveRows / 2 : kWaveRows);
+  u.n0 = (w - tile * blocks) * rows;
   if (a.ids == nullptr) {
     const int per = (static_cast<int>(a.n_tokens) + TILE - 1) / TILE;
     u.h = tile / per;
@@ -489,42 +608,59 @@ __global__ __launch_bounds__(256, 2) void i8_tiles(I8Args a, Plan p, int blocks,
     u.count = static_cast<int>(a.n_tokens) - u.first;
   } else {
     const int2 t = p.tiles[tile];
-    u.h = t.x;
-    u.first = t.y;
-    if (u.h < 0) return;
-    u.count = p.first[u.h + 1] - u.first;
+    u.h = __builtin_amdgcn_readfirstlane(t.x);
+    u.first = __builtin_amdgcn_readfirstlane(t.y);
+    if (u.h < 0) return false;
+    u.count = __builtin_amdgcn_readfirstlane(p.first[u.h + 1]) - u.first;
   }
   u.count = min(u.count, TILE);
+  return true;
+}
+
+// grid: tiles of pairs x blocks of output columns, then `clear` workgroups.
+__global__ __launch_bounds__(256, 2) void i8_tiles(I8Args a, Plan p, int blocks, int rows, int clear) {
+  __shared__ alignas(16) char lds[2 * (kManyTile / 16) * 1024];
+  Unit u;
+  if (!unit_of<kManyTile>(a, p, blocks, rows, clear, u)) return;
   const int jt = (u.count + 15) / 16;
-  if constexpr (TILE >= 128) {
-    if (jt > 6) return tile_product<8>(a, p, u, lds);
-    if (jt > 4) return tile_product<6>(a, p, u, lds);
-    if (jt > 2) return tile_product<4>(a, p, u, lds);
-  }
-  if (jt > 1) return tile_product<2>(a, p, u, lds);
-  tile_product<1>(a, p, u, lds);
+  if (jt > 6) tile_product<8>(a, p, u, lds);
+  else if (jt > 4) tile_product<6>(a, p, u, lds);
+  else if (jt > 2) tile_product<4>(a, p, u, lds);
+  else tile_product<2>(a, p, u, lds);
+}
+
+template <int RF, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void i8_stream(I8Args a, Plan p, int blocks, int rows, int clear) {
+  __shared__ int4v lds[SPLIT ? (kWaves - 1) * RF * 2 * 64 : 1];
+  Unit u;
+  if (!unit_of<kFewTile>(a, p, blocks, rows, clear, u)) return;
+  if (u.count > 16) stream_product<RF, 2, SPLIT>(a, p, u, lds);
+  else stream_product<RF, 1, SPLIT>(a, p, u, lds);
 }
 
 // Sums over the slots of a token, in order.  grid: (blocks of 1024 output columns, tokens).
 __global__ __launch_bounds__(256) void i8_combine(I8Args a) {
-  const int n = (blockIdx.x * 256 + threadIdx.x) * 4;
-  if (n >= a.N) return;
+  const int n = (blockIdx.x * 256 + threadIdx.x) * 4, lane = threadIdx.x & 63;
   for (int64_t t = blockIdx.y; t < a.n_tokens; t += gridDim.y) {
+    // a lane per slot: which are served here, and their gates
+    const int64_t own = t * a.k + min(lane, a.k - 1);
+    const float gate = a.gate != nullptr ? a.gate[own] : 1.0f;
+    uint64_t served = __ballot(lane < a.k && place_of(a, own, lane) >= 0);
     float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j = 0; j < a.k; ++j) {
-      const int64_t pair = t * a.k + j;
-      if (place_of(a, pair, j) < 0) continue;
-      const float g = a.gate != nullptr ? a.gate[pair] : 1.0f;
-      const float* v = a.part + pair * a.N + n;
+    while (served != 0) {
+      const int j = __ffsll(static_cast<unsigned long long>(served)) - 1;
+      served &= served - 1;
+      const float g = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(gate), j));
+      const float* v = a.part + (t * a.k + j) * a.N + n;
       float f[4];
-      if (a.N % 4 == 0) __builtin_memcpy(f, v, 16);
+      if (n + 4 <= a.N) __builtin_memcpy(f, v, 16);
       else
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = n + i < a.N ? v[i] : 0.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] += g * f[i];
     }
-    put(a, t, n, a.N, y, a.out, a.out_dtype);
+    if (n < a.N) put(a, t, n, a.N, y, a.out, a.out_dtype);
   }
 }
 
@@ -560,8 +696,8 @@ TokenArgs token_args(const void* x, int64_t stride_token, int64_t stride_slot, i
   return t;
 }
 
-// Pairs of a tile: as many as there are weight rows to share them with, unless few pairs fall to a matrix.
-int tile_of(int64_t pairs, int32_t n_held) { return pairs > 24 * static_cast<int64_t>(n_held) ? 128 : 32; }
+// Whether so few pairs fall to a matrix, on average, that their time is that of the weights' loads.
+bool few_pairs(int64_t pairs, int32_t n_experts) { return pairs <= 24 * static_cast<int64_t>(n_experts); }
 
 // The parts of a call's workspace.
 struct Space {
@@ -572,7 +708,7 @@ struct Space {
   size_t bytes;
 };
 
-Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
+Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
                bool slots) {
   Space s{};
   Carver ws{static_cast<char*>(base), 0};
@@ -581,7 +717,7 @@ Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_held, int3
     s.levels = ws.take<int8_t>(rows * ((n_cols + kTileCols - 1) / kTileCols * kTileCols));
     s.scales = ws.take<float>(rows);
   }
-  s.plan.tile = tile_of(pairs, n_held);
+  s.plan.tile = few_pairs(pairs, n_experts) ? kFewTile : kManyTile;
   s.plan.n_tiles = static_cast<int32_t>(pairs / s.plan.tile + n_held);
   s.plan.order = ws.take<int32_t>(pairs);
   s.plan.first = ws.take<int32_t>(n_held + 2);
@@ -618,9 +754,9 @@ int launch_token_i8(const void* x, int32_t dtype, int64_t row_stride, int64_t n_
   return hipGetLastError() == hipSuccess ? TACG_OK : TACG_E_DEVICE;
 }
 
-size_t expert_i8_workspace(int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
-                           bool slots) {
-  return space_of(nullptr, n_tokens, top_k, n_held, n_rows, n_cols, mode, dtype, slots).bytes;
+size_t expert_i8_workspace(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols,
+                           int32_t mode, int32_t dtype, bool slots) {
+  return space_of(nullptr, n_tokens, top_k, n_experts, n_held, n_rows, n_cols, mode, dtype, slots).bytes;
 }
 
 int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
@@ -628,7 +764,7 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
                      const int8_t* w, const float* w_scale, int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate,
                      void* out, int32_t out_dtype, uint32_t* d_err, void* workspace, hipStream_t stream) {
   const bool slots = stride_slot != 0;
-  Space s = space_of(workspace, n_tokens, top_k, n_held, n_rows, n_cols, mode, dtype, slots);
+  Space s = space_of(workspace, n_tokens, top_k, ids != nullptr ? n_experts : n_held, n_held, n_rows, n_cols, mode, dtype, slots);
   I8Args a{};
   a.n_tokens = n_tokens;
   a.k = top_k;
@@ -648,7 +784,17 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
   a.part = s.part;
   a.out = out;
   a.err = d_err;
-  const int width = mode == TACG_Q4_GLU ? n_rows / 2 : n_rows, per = kWaves * (mode == TACG_Q4_GLU ? kWaveRows / 2 : kWaveRows);
+  // rows of a workgroup: fewer where the grid would leave processors idle
+  const bool few = s.plan.tile == kFewTile;
+  const int64_t busy = ids == nullptr ? (n_tokens + s.plan.tile - 1) / s.plan.tile * n_held
+                                      : std::min<int64_t>(n_tokens * top_k, n_held + n_tokens * top_k / s.plan.tile);
+  int frags = 4 * kWaves;
+  bool split = false;
+  if (few) {
+    if (busy * n_rows < 256 * 8 * 64) frags = 2, split = true;
+    else if (busy * n_rows < 256 * 12 * 64) frags = 2 * kWaves;
+  }
+  const int width = mode == TACG_Q4_GLU ? n_rows / 2 : n_rows, per = frags * kTileRows / (mode == TACG_Q4_GLU ? 2 : 1);
   const int blocks = (width + per - 1) / per;
   if (ids == nullptr) s.plan.n_tiles = static_cast<int>((n_tokens + s.plan.tile - 1) / s.plan.tile) * n_held;
   const int clear = ids != nullptr && s.part == nullptr ? static_cast<int>(std::min<int64_t>(n_tokens * top_k, 256)) : 0;
@@ -673,8 +819,8 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
   }
   if (hipGetLastError() != hipSuccess) return TACG_E_DEVICE;
   if (grid > 0) {
-    if (s.plan.tile == 128) i8_tiles<128><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(a, s.plan, blocks, clear);
-    else i8_tiles<32><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(a, s.plan, blocks, clear);
+    auto* kernel = !few ? i8_tiles : split ? i8_stream<2, true> : frags == 2 * kWaves ? i8_stream<2, false> : i8_stream<4, false>;
+    kernel<<<static_cast<uint32_t>(grid), 256, 0, stream>>>(a, s.plan, blocks, per, clear);
   }
   if (s.part != nullptr) {
     const dim3 sums((n_rows + 1023) / 1024, static_cast<uint32_t>(std::min<int64_t>(n_tokens, 65535)));

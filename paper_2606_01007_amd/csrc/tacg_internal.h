@@ -135,8 +135,8 @@ int launch_i8_pack(const void* w, int32_t dtype, int64_t n_matrices, int32_t n_r
                    uint32_t* d_err, hipStream_t stream);
 int launch_token_i8(const void* x, int32_t dtype, int64_t row_stride, int64_t n_rows, int32_t n_cols, int8_t* q, float* scale,
                     uint32_t* d_err, hipStream_t stream);
-size_t expert_i8_workspace(int64_t n_tokens, int32_t top_k, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
-                           bool slots);
+size_t expert_i8_workspace(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols,
+                           int32_t mode, int32_t dtype, bool slots);
 int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
                      int32_t top_k, int32_t n_experts, const int16_t* ids, const int32_t* slot_of_expert, int32_t n_held,
                      const int8_t* w, const float* w_scale, int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate,

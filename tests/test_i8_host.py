@@ -99,11 +99,11 @@ def test_products_refuse(L):
 
 def test_workspace(L):
     need = lambda *a: L.tacg_expert_i8_workspace_bytes(*a)  # noqa: E731
-    assert need(4, 2, 8, 16, 64, 0, 1, 0) % 256 == 0
-    assert need(4, 2, 8, 16, 64, 0, 1, 0) >= 4 * 64 + 16
-    assert need(4, 2, 8, 16, 65, 2, 1, 1) >= 8 * 128 + 32
-    for bad in ((-1, 2, 8, 16, 64, 0, 1, 0), (4, 0, 8, 16, 64, 0, 1, 0), (4, 2, -1, 16, 64, 0, 1, 0), (4, 2, 8, 0, 64, 0, 1, 0),
-                (4, 2, 8, 16, 0, 0, 1, 0)):
+    assert need(4, 2, 8, 8, 16, 64, 0, 1, 0) % 256 == 0
+    assert need(4, 2, 8, 8, 16, 64, 0, 1, 0) >= 4 * 64 + 16
+    assert need(4, 2, 8, 8, 16, 65, 2, 1, 1) >= 8 * 128 + 32
+    for bad in ((-1, 2, 8, 8, 16, 64, 0, 1, 0), (4, 0, 8, 8, 16, 64, 0, 1, 0), (4, 2, -1, 8, 16, 64, 0, 1, 0), (4, 2, 8, -1, 16, 64, 0, 1, 0),
+                (4, 2, 8, 8, 0, 64, 0, 1, 0), (4, 2, 8, 8, 16, 0, 0, 1, 0)):
         assert need(*bad) == 0
 
 

@@ -26,6 +26,7 @@ struct I8Args {
   int64_t x_token, x_slot;  // strides of the levels, in bytes
   int64_t n_tokens;
   int32_t k, E, H, N, row_tiles, col_tiles, mode, out_dtype, slots;  // slots: whether every slot has its own x
+  uint32_t over_k;          // the high half of pair * over_k is pair / k (0 for k = 1): pairs are below 2^27, k up to 16
   const int16_t* ids;       // or null: slot j takes matrix j
   const int32_t* slot;      // [E] or null
   const int8_t* w;
@@ -35,6 +36,10 @@ struct I8Args {
   void* out;
   uint32_t* err;
 };
+
+__device__ __forceinline__ int token_index(const I8Args& a, int pair) {
+  return a.over_k != 0 ? static_cast<int>(__umulhi(static_cast<uint32_t>(pair), a.over_k)) : pair;
+}
 
 constexpr int kBadId = -2, kBadTable = -3;
 
@@ -203,23 +208,27 @@ __global__ __launch_bounds__(256) void i8_pack_kernel(PackArgs a) {
 
 // Pairs by their matrix: order[first[h] .. first[h + 1]) are those of matrix h, order[first[H] ..) those that are served elsewhere.  The
 // tiles of `tile` pairs of matrix h have the numbers first[h] / tile + h and following: no two matrices share one, and no matrix
-// needs to know the others' tiles.  tiles[i] = matrix and first pair of tile i, or -1.
+// needs to know the others' tiles (with fewer pairs than matrices, first[h] and following).  tiles[i] = matrix and first pair of tile i, or -1.
 struct Plan {
   int32_t* order;
   int32_t* first;     // [H + 2]
   int2* tiles;
   int32_t tile, n_tiles;
+  int32_t sparse;     // fewer pairs than matrices
+  __host__ __device__ int number(int first, int h) const { return sparse ? first : first / tile + h; }
 };
 
-constexpr int kScan = 8, kBatch = 4, kSegment = 8;  // pairs of a load, loads of a batch, batches whose pairs are remembered
-constexpr int kBatchPairs = 256 * kScan * kBatch, kSegmentPairs = kBatchPairs * kSegment;
+constexpr int kScan = 8, kBatch = 4, kSegment = 2;  // pairs of a load, loads of a batch, batches whose pairs are remembered
+
 
 // One workgroup per matrix (and one for what is served elsewhere) looks through all pairs: none waits for another, and no launch is
-// needed to add up counts.  Up to 65536 pairs are read once, with a bit in LDS for each; more are read twice.
+// needed to add up counts.  Up to 64 pairs a lane are read once, with a bit in LDS for each; more are read twice.
+template <int THREADS>
 __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
+  constexpr int kBatchPairs = THREADS * kScan * kBatch, kSegmentPairs = kBatchPairs * kSegment;
   __shared__ int place[TACG_MAX_EXPERTS];
   __shared__ int lower, equal, cursor;
-  __shared__ uint32_t own[kSegment][256];  // a lane reads what it wrote itself
+  __shared__ uint32_t own[kSegment][THREADS];  // a lane reads what it wrote itself
   const int tid = threadIdx.x;
   const int pairs = static_cast<int>(a.n_tokens * a.k);
   if (tid == 0) lower = equal = cursor = 0;
@@ -235,7 +244,7 @@ __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
     int4v id[kBatch];  // eight ids each
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int at = base + (i * 256 + tid) * kScan;
+      const int at = base + (i * THREADS + tid) * kScan;
       id[i] = int4v{-1, -1, -1, -1};
       if (at + kScan <= pairs) __builtin_memcpy(&id[i], a.ids + at, 16);
       else if (at < pairs)
@@ -246,7 +255,7 @@ __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int at = base + (i * 256 + tid) * kScan;
+      const int at = base + (i * THREADS + tid) * kScan;
 #pragma unroll
       for (int e = 0; e < kScan; ++e) {
         const int id16 = e % 2 ? id[i][e / 2] >> 16 : static_cast<int16_t>(id[i][e / 2]);
@@ -285,12 +294,12 @@ __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
   for (int base = 0; base < pairs && count > 0; base += kBatchPairs) {
     for (uint32_t m = pairs > kSegmentPairs ? batch(base) : own[base / kBatchPairs][tid]; m != 0; m &= m - 1) {
       const int bit = __ffs(m) - 1;
-      p.order[at++] = base + (bit / kScan * 256 + tid) * kScan + bit % kScan;
+      p.order[at++] = base + (bit / kScan * THREADS + tid) * kScan + bit % kScan;
     }
   }
-  const int begin = from / p.tile + h;
-  const int end = h < a.H ? (from + count) / p.tile + h + 1 : p.n_tiles;
-  for (int i = begin + tid; i < end; i += 256) {
+  const int begin = p.number(from, h);
+  const int end = h < a.H ? p.number(from + count, h + 1) : p.n_tiles;
+  for (int i = begin + tid; i < end; i += THREADS) {
     const int start = from + (i - begin) * p.tile;
     p.tiles[i] = h < a.H && start < from + count ? make_int2(h, start) : make_int2(-1, 0);
   }
@@ -300,16 +309,16 @@ __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
   }
 }
 
-// grid: n_plan workgroups for the order of the pairs, then workgroups of four waves, a row of tokens each.
-template <int DTYPE, int CH>
-__global__ __launch_bounds__(256) void i8_prepare(TokenArgs t, I8Args a, Plan p, int n_plan, bool skip) {
+// grid: n_plan workgroups for the order of the pairs, then workgroups whose waves take a row of tokens each.
+template <int DTYPE, int CH, int THREADS>
+__global__ __launch_bounds__(THREADS) void i8_prepare(TokenArgs t, I8Args a, Plan p, int n_plan, bool skip) {
   if (static_cast<int>(blockIdx.x) < n_plan) {
-    plan_block(a, p, blockIdx.x);
+    plan_block<THREADS>(a, p, blockIdx.x);
     return;
   }
   const int lane = threadIdx.x & 63;
-  const int64_t step = static_cast<int64_t>(gridDim.x - n_plan) * 4;
-  for (int64_t r = static_cast<int64_t>(blockIdx.x - n_plan) * 4 + (threadIdx.x >> 6); r < t.rows; r += step)
+  const int64_t step = static_cast<int64_t>(gridDim.x - n_plan) * (THREADS / 64);
+  for (int64_t r = static_cast<int64_t>(blockIdx.x - n_plan) * (THREADS / 64) + (threadIdx.x >> 6); r < t.rows; r += step)
     if (!skip || place_of(a, r, 0) >= 0) round_row<DTYPE, CH>(t, r, lane);
 }
 
@@ -349,8 +358,8 @@ struct Unit {
   int n0;               // first output column
 };
 
-__device__ __forceinline__ int64_t pair_of(const I8Args& a, const Plan& p, const Unit& u, int i) {
-  return a.ids == nullptr ? static_cast<int64_t>(u.first + i) * a.k + u.h : p.order[u.first + i];
+__device__ __forceinline__ int pair_of(const I8Args& a, const Plan& p, const Unit& u, int i) {
+  return a.ids == nullptr ? (u.first + i) * a.k + u.h : p.order[u.first + i];
 }
 
 // Where a lane's piece of a block of 16 weight rows lies in its matrix: its row's 16 bytes of the tile's first 64 columns.  Gated: RF / 2
@@ -369,8 +378,9 @@ __device__ __forceinline__ void weight_rows(const I8Args& a, int n0, bool glu, i
 __device__ __forceinline__ const char* matrix_of(const I8Args& a, int h) {
   return reinterpret_cast<const char*>(a.w) + static_cast<int64_t>(h) * a.row_tiles * a.col_tiles * kTileBytes;
 }
-__device__ __forceinline__ const int8_t* token_of(const I8Args& a, int64_t pair) {
-  return a.x + pair / a.k * a.x_token + pair % a.k * a.x_slot + ((threadIdx.x & 63) >> 4) * kPiece;
+__device__ __forceinline__ const int8_t* token_of(const I8Args& a, int pair) {
+  const int t = token_index(a, pair);
+  return a.x + t * a.x_token + (pair - t * a.k) * a.x_slot + ((threadIdx.x & 63) >> 4) * kPiece;
 }
 __device__ __forceinline__ int4v load16(const void* p) { return *static_cast<const int4v*>(p); }
 
@@ -378,50 +388,59 @@ __device__ __forceinline__ int4v load16(const void* p) { return *static_cast<con
 template <int RF, int JT>
 __device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Unit& u, int n0, const int4v (&acc)[RF][JT]) {
   const int lane = threadIdx.x & 63;
-  const bool glu = a.mode == TACG_Q4_GLU, sum = a.mode == TACG_Q4_SUM;
+  const bool glu = a.mode == TACG_Q4_GLU;
   const int width = glu ? a.N / 2 : a.N;
   const float* sw = a.w_scale + static_cast<int64_t>(u.h) * a.N;
+  float scale[RF][4];
+#pragma unroll
+  for (int i = 0; i < RF; ++i) {
+    const int n = n0 + (glu ? i / 2 : i) * kTileRows + (lane >> 4) * 4;
+    const float* from = sw + (glu && (i & 1) ? width : 0);
+    if (n + 4 <= width) __builtin_memcpy(scale[i], from + n, 16);
+    else
+#pragma unroll
+      for (int r = 0; r < 4; ++r) scale[i][r] = from[min(n + r, width - 1)];
+  }
+  const bool part = a.mode == TACG_Q4_SUM && a.part != nullptr;
+  void* out = part ? a.part : a.out;
+  const int dtype = part ? TACG_F32 : a.out_dtype;
 #pragma unroll
   for (int j = 0; j < JT; ++j) {
     const int i0 = j * 16 + (lane & 15);
     if (i0 >= u.count) continue;
-    const int64_t pair = pair_of(a, p, u, i0);
-    const float sx = a.x_scale[a.slots ? pair : pair / a.k];
-    const float gate = sum && a.part == nullptr && a.gate != nullptr ? a.gate[pair] : 1.0f;
-    auto scaled = [&](int sum32, int row) { return static_cast<float>(sum32) * (sx * sw[row]); };
+    const int pair = pair_of(a, p, u, i0);
+    const float sx = a.x_scale[a.slots ? pair : token_index(a, pair)];
+    const float gate = a.mode == TACG_Q4_SUM && !part && a.gate != nullptr ? a.gate[pair] : 1.0f;
     if (glu) {
       if constexpr (RF > 1) {
 #pragma unroll
         for (int i = 0; i < RF / 2; ++i) {
           const int n = n0 + i * kTileRows + (lane >> 4) * 4;
-          if (n >= width) continue;
           float y[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int row = min(n + r, width - 1);
-            const float g = scaled(acc[2 * i][j][r], row);
-            y[r] = g / (1.0f + __expf(-g)) * scaled(acc[2 * i + 1][j][r], row + width);
+            const float g = static_cast<float>(acc[2 * i][j][r]) * (sx * scale[2 * i][r]);
+            const float v = static_cast<float>(acc[2 * i + 1][j][r]) * (sx * scale[2 * i + 1][r]);
+            y[r] = g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * v;  // the reciprocal is within one unit in the last place
           }
-          put(a, pair, n, width, y, a.out, a.out_dtype);
+          if (n < width) put(a, pair, n, width, y, out, dtype);
         }
       }
-      continue;
-    }
+    } else {
 #pragma unroll
-    for (int i = 0; i < RF; ++i) {
-      const int n = n0 + i * kTileRows + (lane >> 4) * 4;
-      if (n >= width) continue;
-      float y[4];
+      for (int i = 0; i < RF; ++i) {
+        const int n = n0 + i * kTileRows + (lane >> 4) * 4;
+        float y[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = scaled(acc[i][j][r], min(n + r, width - 1)) * gate;
-      if (sum && a.part != nullptr) put(a, pair, n, width, y, a.part, TACG_F32);
-      else put(a, pair, n, width, y, a.out, a.out_dtype);
+        for (int r = 0; r < 4; ++r) y[r] = static_cast<float>(acc[i][j][r]) * (sx * scale[i][r]) * gate;
+        if (n < width) put(a, pair, n, width, y, out, dtype);
+      }
     }
   }
 }
 
 // Many tokens: a wave has 64 weight rows and all tokens of the tile, JT blocks of 16.  Steps of 64 columns: weights go from memory to the
-// registers of the wave that needs them, two steps ahead; tokens through LDS, one step ahead, and from there two blocks ahead.
+// registers of the wave that needs them, three steps ahead; tokens through LDS, two steps ahead, and from there two blocks ahead.
 template <int JT>
 __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, const Unit& u, char* lds) {
   constexpr int RF = 4, kLoads = (JT + kWaves - 1) / kWaves;  // blocks of tokens that a wave brings in a step
@@ -447,27 +466,28 @@ __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, con
 #pragma unroll
     for (int i = 0; i < RF; ++i) v[i] = load16(w + (at[i] + from));
   };
-  int4v tk[kLoads];
-  auto load_tokens = [&](int c) {
+  auto load_tokens = [&](int c, int4v (&v)[kLoads]) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) tk[i] = load16(token[i] + min(c, last) * kTileCols);
+    for (int i = 0; i < kLoads; ++i) v[i] = load16(token[i] + min(c, last) * kTileCols);
   };
-  auto keep_tokens = [&](int c) {
+  auto keep_tokens = [&](int c, const int4v (&v)[kLoads]) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int j = wave + i * kWaves;
-      if (JT % kWaves == 0 || j < JT) *reinterpret_cast<int4v*>(lds + (c & 1) * kStage + j * 1024 + lane * 16) = tk[i];
+      if (JT % kWaves == 0 || j < JT) *reinterpret_cast<int4v*>(lds + (c & 1) * kStage + j * 1024 + lane * 16) = v[i];
     }
   };
-  int4v w0[RF], w1[RF], w2[RF];
-  load_tokens(0);
+  int4v w0[RF], w1[RF], w2[RF], w3[RF], t0[kLoads], t1[kLoads];
+  load_tokens(0, t0);
   load_weights(0, w0);
+  load_tokens(1, t1);
   load_weights(1, w1);
-  keep_tokens(0);
-  auto step = [&](int c, int4v (&now)[RF], int4v (&far)[RF]) {
+  load_weights(2, w2);
+  keep_tokens(0, t0);
+  auto step = [&](int c, int4v (&now)[RF], int4v (&far)[RF], int4v (&after)[kLoads], const int4v (&next)[kLoads]) {
     __syncthreads();
-    load_tokens(c + 1);
-    load_weights(c + 2, far);
+    load_tokens(c + 2, after);
+    load_weights(c + 3, far);
     const char* from = lds + (c & 1) * kStage + lane * 16;
     int4v t[2];
     t[0] = load16(from);
@@ -480,15 +500,17 @@ __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, con
       if (j + 2 < JT) t[j & 1] = load16(from + (j + 2) * 1024);
     }
     __builtin_amdgcn_sched_barrier(0);
-    keep_tokens(c + 1);
+    keep_tokens(c + 1, next);
   };
-  for (int c = 0;; c += 3) {
-    step(c, w0, w2);
+  for (int c = 0;; c += 4) {
+    step(c, w0, w3, t0, t1);
     if (c + 1 > last) break;
-    step(c + 1, w1, w0);
+    step(c + 1, w1, w0, t1, t0);
     if (c + 2 > last) break;
-    step(c + 2, w2, w1);
+    step(c + 2, w2, w1, t0, t1);
     if (c + 3 > last) break;
+    step(c + 3, w3, w2, t1, t0);
+    if (c + 4 > last) break;
   }
   finish<RF, JT>(a, p, u, n0, acc);
 }
@@ -590,7 +612,7 @@ __device__ __forceinline__ void clear_block(const I8Args& a, const Plan& p, int 
 template <int TILE>
 __device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int blocks, int rows, int clear, Unit& u) {
   // tiles that there are: those of pairs served here
-  const int total = (a.ids == nullptr ? p.n_tiles : __builtin_amdgcn_readfirstlane(p.first[a.H]) / TILE + a.H) * blocks;
+  const int total = (a.ids == nullptr ? p.n_tiles : p.number(__builtin_amdgcn_readfirstlane(p.first[a.H]), a.H)) * blocks;
   int w = blockIdx.x;
   if (w >= total) {
     const int all = p.n_tiles * blocks;
@@ -664,14 +686,23 @@ __global__ __launch_bounds__(256) void i8_combine(I8Args a) {
   }
 }
 
+template <int DTYPE, int THREADS>
+void start_prepare(const TokenArgs& t, const I8Args& a, const Plan& p, int n_plan, bool skip, hipStream_t stream) {
+  constexpr int kRows = THREADS / 64;
+  const dim3 grid(static_cast<uint32_t>(n_plan + std::min<int64_t>((t.rows + kRows - 1) / kRows, 1 << 20)));
+  auto* kernel = t.K <= kWaveChunk       ? i8_prepare<DTYPE, 1, THREADS>
+                 : t.K <= 2 * kWaveChunk ? i8_prepare<DTYPE, 2, THREADS>
+                 : t.K <= 4 * kWaveChunk ? i8_prepare<DTYPE, 4, THREADS>
+                 : t.K <= 8 * kWaveChunk ? i8_prepare<DTYPE, 8, THREADS>
+                                         : i8_prepare<DTYPE, 0, THREADS>;
+  kernel<<<grid, THREADS, 0, stream>>>(t, a, p, n_plan, skip);
+}
+
+// Many pairs are looked through by more threads.
 template <int DTYPE>
 void start_prepare(const TokenArgs& t, const I8Args& a, const Plan& p, int n_plan, bool skip, hipStream_t stream) {
-  const dim3 grid(static_cast<uint32_t>(n_plan + std::min<int64_t>((t.rows + 3) / 4, 1 << 20)));
-  if (t.K <= kWaveChunk) i8_prepare<DTYPE, 1><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
-  else if (t.K <= 2 * kWaveChunk) i8_prepare<DTYPE, 2><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
-  else if (t.K <= 4 * kWaveChunk) i8_prepare<DTYPE, 4><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
-  else if (t.K <= 8 * kWaveChunk) i8_prepare<DTYPE, 8><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
-  else i8_prepare<DTYPE, 0><<<grid, 256, 0, stream>>>(t, a, p, n_plan, skip);
+  if (n_plan > 0 && a.n_tokens * a.k > 8192) start_prepare<DTYPE, 1024>(t, a, p, n_plan, skip, stream);
+  else start_prepare<DTYPE, 256>(t, a, p, n_plan, skip, stream);
 }
 
 void start_prepare(const TokenArgs& t, int32_t dtype, const I8Args& a, const Plan& p, int n_plan, bool skip, hipStream_t stream) {
@@ -718,7 +749,8 @@ Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_experts, i
     s.scales = ws.take<float>(rows);
   }
   s.plan.tile = few_pairs(pairs, n_experts) ? kFewTile : kManyTile;
-  s.plan.n_tiles = static_cast<int32_t>(pairs / s.plan.tile + n_held);
+  s.plan.sparse = pairs <= n_held;
+  s.plan.n_tiles = s.plan.sparse ? static_cast<int32_t>(pairs) : static_cast<int32_t>(pairs / s.plan.tile + n_held);
   s.plan.order = ws.take<int32_t>(pairs);
   s.plan.first = ws.take<int32_t>(n_held + 2);
   s.plan.tiles = ws.take<int2>(s.plan.n_tiles);
@@ -768,6 +800,7 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
   I8Args a{};
   a.n_tokens = n_tokens;
   a.k = top_k;
+  a.over_k = top_k > 1 ? static_cast<uint32_t>((0x100000000u + top_k - 1) / top_k) : 0;
   a.E = n_experts;
   a.H = n_held;
   a.N = n_rows;

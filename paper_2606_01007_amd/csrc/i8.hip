@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
+#include <utility>
 
 #include "tacg_internal.h"
 
@@ -206,12 +207,12 @@ __global__ __launch_bounds__(256) void i8_pack_kernel(PackArgs a) {
 
 // ---- the order of the pairs -------------------------------------------------------------------
 
-// Pairs by their matrix: order[first[h] .. first[h + 1]) are those of matrix h, order[first[H] ..) those that are served elsewhere.  The
+// The pairs served here by their matrix: order[first[h] .. first[h + 1]) are those of matrix h.  The
 // tiles of `tile` pairs of matrix h have the numbers first[h] / tile + h and following: no two matrices share one, and no matrix
-// needs to know the others' tiles (with fewer pairs than matrices, first[h] and following).  tiles[i] = matrix and first pair of tile i, or -1.
+// needs to know the others' tiles (with fewer pairs than matrices, first[h] and following).  tiles[i] = matrix and first pair of tile i, or -1, up to number(first[H], H).
 struct Plan {
   int32_t* order;
-  int32_t* first;     // [H + 2]
+  int32_t* first;     // [H + 1]
   int2* tiles;
   int32_t tile, n_tiles;
   int32_t sparse;     // fewer pairs than matrices
@@ -221,7 +222,7 @@ struct Plan {
 constexpr int kScan = 8, kBatch = 4, kSegment = 2;  // pairs of a load, loads of a batch, batches whose pairs are remembered
 
 
-// One workgroup per matrix (and one for what is served elsewhere) looks through all pairs: none waits for another, and no launch is
+// One workgroup per matrix looks through all pairs: none waits for another, and no launch is
 // needed to add up counts.  Up to 64 pairs a lane are read once, with a bit in LDS for each; more are read twice.
 template <int THREADS>
 __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
@@ -264,8 +265,7 @@ __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
         if (!in) v = id16 == -1 ? -1 : kBadId;
         bad |= v == kBadId ? TACG_ERR_ID_RANGE : v == kBadTable ? TACG_ERR_TABLE : 0u;
         below += v >= 0 && v < h;
-        const bool is = at + e < pairs && (h < a.H ? v == h : v < 0);
-        mine |= static_cast<uint32_t>(is) << (i * kScan + e);
+        mine |= static_cast<uint32_t>(v == h) << (i * kScan + e);  // pairs past the last have the id -1
       }
     }
     return mine;
@@ -298,28 +298,36 @@ __device__ void plan_block(const I8Args& a, const Plan& p, int h) {
     }
   }
   const int begin = p.number(from, h);
-  const int end = h < a.H ? p.number(from + count, h + 1) : p.n_tiles;
+  const int end = h < a.H ? p.number(from + count, h + 1) : begin;  // without any matrix there are no tiles
   for (int i = begin + tid; i < end; i += THREADS) {
     const int start = from + (i - begin) * p.tile;
-    p.tiles[i] = h < a.H && start < from + count ? make_int2(h, start) : make_int2(-1, 0);
+    p.tiles[i] = start < from + count ? make_int2(h, start) : make_int2(-1, 0);
   }
   if (tid == 0) {
     p.first[h] = from;
-    if (h == a.H) p.first[h + 1] = from + count;
+    if (h == a.H - 1) p.first[a.H] = from + count;
   }
 }
 
-// grid: n_plan workgroups for the order of the pairs, then workgroups whose waves take a row of tokens each.
+// grid: n_plan workgroups for the order of the pairs, then workgroups whose waves take a row of tokens each, or (skip > 0, rows are pairs)
+// those of `skip` rows that are served here.
 template <int DTYPE, int CH, int THREADS>
-__global__ __launch_bounds__(THREADS) void i8_prepare(TokenArgs t, I8Args a, Plan p, int n_plan, bool skip) {
+__global__ __launch_bounds__(THREADS) void i8_prepare(TokenArgs t, I8Args a, Plan p, int n_plan, int skip) {
   if (static_cast<int>(blockIdx.x) < n_plan) {
     plan_block<THREADS>(a, p, blockIdx.x);
     return;
   }
   const int lane = threadIdx.x & 63;
   const int64_t step = static_cast<int64_t>(gridDim.x - n_plan) * (THREADS / 64);
-  for (int64_t r = static_cast<int64_t>(blockIdx.x - n_plan) * (THREADS / 64) + (threadIdx.x >> 6); r < t.rows; r += step)
-    if (!skip || place_of(a, r, 0) >= 0) round_row<DTYPE, CH>(t, r, lane);
+  const int64_t own = static_cast<int64_t>(blockIdx.x - n_plan) * (THREADS / 64) + (threadIdx.x >> 6);
+  if (skip == 0) {
+    for (int64_t r = own; r < t.rows; r += step) round_row<DTYPE, CH>(t, r, lane);
+    return;
+  }
+  for (int64_t base = own * skip; base < t.rows; base += step * skip) {
+    uint64_t served = __ballot(lane < skip && base + lane < t.rows && place_of(a, min(base + lane, t.rows - 1), 0) >= 0);
+    for (; served != 0; served &= served - 1) round_row<DTYPE, CH>(t, base + __ffsll(static_cast<unsigned long long>(served)) - 1, lane);
+  }
 }
 
 // ---- products ----------------------------------------------------------------------------------
@@ -327,6 +335,9 @@ __global__ __launch_bounds__(THREADS) void i8_prepare(TokenArgs t, I8Args a, Pla
 constexpr int kManyTile = 128, kFewTile = 32;  // pairs of a tile
 
 constexpr int kWaves = 4;
+// A block of 16 tokens in LDS: 16 bytes of each after another, for each quarter of the 64 columns; quarters are 18 * 16 bytes apart, so that
+// eight lanes that write all quarters of two tokens meet no bank twice.
+constexpr int kPieceBytes = 18 * 16, kBlockBytes = 4 * kPieceBytes;
 
 // What a lane does of its part of a tile's results: 4 consecutive rows of a token.
 __device__ __forceinline__ void put(const I8Args& a, int64_t row, int n, int width, const float (&y)[4], void* out, int dtype) {
@@ -380,9 +391,15 @@ __device__ __forceinline__ const char* matrix_of(const I8Args& a, int h) {
 }
 __device__ __forceinline__ const int8_t* token_of(const I8Args& a, int pair) {
   const int t = token_index(a, pair);
-  return a.x + t * a.x_token + (pair - t * a.k) * a.x_slot + ((threadIdx.x & 63) >> 4) * kPiece;
+  return a.x + t * a.x_token + (pair - t * a.k) * a.x_slot;
 }
 __device__ __forceinline__ int4v load16(const void* p) { return *static_cast<const int4v*>(p); }
+
+// f(integral_constant 0), f(1), ... f(N - 1): what a loop of so many steps is not unrolled to.
+template <class F, int... I>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>()), ...);
+}
 
 // Results of a wave: lane n + 16 q holds rows 4 q .. 4 q + 3 of a block for token n.
 template <int RF, int JT>
@@ -404,10 +421,10 @@ __device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Uni
   const bool part = a.mode == TACG_Q4_SUM && a.part != nullptr;
   void* out = part ? a.part : a.out;
   const int dtype = part ? TACG_F32 : a.out_dtype;
-#pragma unroll
-  for (int j = 0; j < JT; ++j) {
+  each_of(std::make_integer_sequence<int, JT>(), [&](auto block) {
+    constexpr int j = decltype(block)::value;
     const int i0 = j * 16 + (lane & 15);
-    if (i0 >= u.count) continue;
+    if (i0 >= u.count) return;
     const int pair = pair_of(a, p, u, i0);
     const float sx = a.x_scale[a.slots ? pair : token_index(a, pair)];
     const float gate = a.mode == TACG_Q4_SUM && !part && a.gate != nullptr ? a.gate[pair] : 1.0f;
@@ -436,15 +453,15 @@ __device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Uni
         if (n < width) put(a, pair, n, width, y, out, dtype);
       }
     }
-  }
+  });
 }
 
 // Many tokens: a wave has 64 weight rows and all tokens of the tile, JT blocks of 16.  Steps of 64 columns: weights go from memory to the
 // registers of the wave that needs them, three steps ahead; tokens through LDS, two steps ahead, and from there two blocks ahead.
 template <int JT>
 __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, const Unit& u, char* lds) {
-  constexpr int RF = 4, kLoads = (JT + kWaves - 1) / kWaves;  // blocks of tokens that a wave brings in a step
-  constexpr int kStage = JT * 1024;
+  constexpr int RF = 4, AHEAD = 2, kLoads = (JT + kWaves - 1) / kWaves;  // blocks of tokens that a wave brings in a step
+  constexpr int kStage = JT * kBlockBytes;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool glu = a.mode == TACG_Q4_GLU;
   const int width = glu ? a.N / 2 : a.N;
@@ -454,7 +471,8 @@ __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, con
   weight_rows<RF>(a, n0, glu, width, at);
   const int8_t* token[kLoads];
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) token[i] = token_of(a, pair_of(a, p, u, min((wave + i * kWaves) * 16 + (lane & 15), u.count - 1)));
+  for (int i = 0; i < kLoads; ++i)  // four neighbouring lanes share a token: 64 bytes of a line at a time
+    token[i] = token_of(a, pair_of(a, p, u, min((wave + i * kWaves) * 16 + (lane >> 2), u.count - 1))) + (lane & 3) * kPiece;
   int4v acc[RF][JT];
 #pragma unroll
   for (int i = 0; i < RF; ++i)
@@ -474,7 +492,8 @@ __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, con
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int j = wave + i * kWaves;
-      if (JT % kWaves == 0 || j < JT) *reinterpret_cast<int4v*>(lds + (c & 1) * kStage + j * 1024 + lane * 16) = v[i];
+      if (JT % kWaves == 0 || j < JT) 
+        *reinterpret_cast<int4v*>(lds + (c & 1) * kStage + j * kBlockBytes + (lane & 3) * kPieceBytes + (lane >> 2) * 16) = v[i];
     }
   };
   int4v w0[RF], w1[RF], w2[RF], w3[RF], t0[kLoads], t1[kLoads];
@@ -488,30 +507,30 @@ __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, con
     __syncthreads();
     load_tokens(c + 2, after);
     load_weights(c + 3, far);
-    const char* from = lds + (c & 1) * kStage + lane * 16;
-    int4v t[2];
-    t[0] = load16(from);
-    if (JT > 1) t[1] = load16(from + 1024);
+    const char* from = lds + (c & 1) * kStage + (lane >> 4) * kPieceBytes + (lane & 15) * 16;
+    int4v t[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) t[j] = load16(from + min(j, JT - 1) * kBlockBytes);
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < RF; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[i], t[j & 1], acc[i][j], 0, 0, 0);
-      if (j + 2 < JT) t[j & 1] = load16(from + (j + 2) * 1024);
+      for (int i = 0; i < RF; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[i], t[j % AHEAD], acc[i][j], 0, 0, 0);
+      if (j + AHEAD < JT) t[j % AHEAD] = load16(from + (j + AHEAD) * kBlockBytes);
     }
     __builtin_amdgcn_sched_barrier(0);
     keep_tokens(c + 1, next);
   };
-  for (int c = 0;; c += 4) {
+  int c = 0;
+  for (; c + 4 <= last + 1; c += 4) {
     step(c, w0, w3, t0, t1);
-    if (c + 1 > last) break;
     step(c + 1, w1, w0, t1, t0);
-    if (c + 2 > last) break;
     step(c + 2, w2, w1, t0, t1);
-    if (c + 3 > last) break;
     step(c + 3, w3, w2, t1, t0);
-    if (c + 4 > last) break;
   }
+  if (c <= last) step(c, w0, w3, t0, t1);
+  if (c + 1 <= last) step(c + 1, w1, w0, t1, t0);
+  if (c + 2 <= last) step(c + 2, w2, w1, t0, t1);
   finish<RF, JT>(a, p, u, n0, acc);
 }
 
@@ -530,7 +549,7 @@ __device__ __forceinline__ void stream_product(const I8Args& a, const Plan& p, c
   weight_rows<RF>(a, n0, glu, width, at);
   const int8_t* token[JT];
 #pragma unroll
-  for (int j = 0; j < JT; ++j) token[j] = token_of(a, pair_of(a, p, u, min(j * 16 + (lane & 15), u.count - 1)));
+  for (int j = 0; j < JT; ++j) token[j] = token_of(a, pair_of(a, p, u, min(j * 16 + (lane & 15), u.count - 1))) + (lane >> 4) * kPiece;
   int4v acc[RF][JT];
 #pragma unroll
   for (int i = 0; i < RF; ++i)
@@ -593,17 +612,21 @@ __device__ __forceinline__ void stream_product(const I8Args& a, const Plan& p, c
   finish<RF, JT>(a, p, u, n0, acc);
 }
 
-// What is served elsewhere is 0.
-__device__ __forceinline__ void clear_block(const I8Args& a, const Plan& p, int block, int blocks) {
+// What is served elsewhere is 0.  A wave takes 64 pairs at a time.
+__device__ __forceinline__ void clear_block(const I8Args& a, int block, int blocks) {
   const int width = a.mode == TACG_Q4_GLU ? a.N / 2 : a.N, size = a.out_dtype == TACG_F32 ? 4 : 2;
   const int64_t bytes = static_cast<int64_t>(width) * size;
-  for (int i = p.first[a.H] + block; i < p.first[a.H + 1]; i += blocks) {
-    char* row = static_cast<char*>(a.out) + p.order[i] * bytes;
-    const int64_t head = min(bytes, static_cast<int64_t>(-reinterpret_cast<uintptr_t>(row) & 15)), body = (bytes - head) / 16;
-    if (threadIdx.x < head / 2) reinterpret_cast<int16_t*>(row)[threadIdx.x] = 0;
-    for (int64_t c = threadIdx.x; c < body; c += 256) reinterpret_cast<int4*>(row + head)[c] = make_int4(0, 0, 0, 0);
-    const int64_t done = head + body * 16;
-    if (threadIdx.x < (bytes - done) / 2) reinterpret_cast<int16_t*>(row + done)[threadIdx.x] = 0;
+  const int lane = threadIdx.x & 63, pairs = static_cast<int>(a.n_tokens) * a.k;
+  for (int base = (block * kWaves + (threadIdx.x >> 6)) * 64; base < pairs; base += blocks * kWaves * 64) {
+    uint64_t away = __ballot(base + lane < pairs && place_of(a, min(base + lane, pairs - 1), 0) < 0);
+    for (; away != 0; away &= away - 1) {
+      char* row = static_cast<char*>(a.out) + (base + __ffsll(static_cast<unsigned long long>(away)) - 1) * bytes;
+      const int64_t head = min(bytes, static_cast<int64_t>(-reinterpret_cast<uintptr_t>(row) & 15)), body = (bytes - head) / 16;
+      if (lane < head / 2) reinterpret_cast<int16_t*>(row)[lane] = 0;
+      for (int64_t c = lane; c < body; c += 64) reinterpret_cast<int4*>(row + head)[c] = make_int4(0, 0, 0, 0);
+      const int64_t done = head + body * 16;
+      if (lane < (bytes - done) / 2) reinterpret_cast<int16_t*>(row + done)[lane] = 0;
+    }
   }
 }
 
@@ -616,7 +639,7 @@ __device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int bloc
   int w = blockIdx.x;
   if (w >= total) {
     const int all = p.n_tiles * blocks;
-    if (w >= all) clear_block(a, p, w - all, clear);
+    if (w >= all) clear_block(a, w - all, clear);
     return false;
   }
   const int share = total / 8;
@@ -641,7 +664,7 @@ __device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int bloc
 
 // grid: tiles of pairs x blocks of output columns, then `clear` workgroups.
 __global__ __launch_bounds__(256, 2) void i8_tiles(I8Args a, Plan p, int blocks, int rows, int clear) {
-  __shared__ alignas(16) char lds[2 * (kManyTile / 16) * 1024];
+  __shared__ alignas(16) char lds[2 * (kManyTile / 16) * kBlockBytes];
   Unit u;
   if (!unit_of<kManyTile>(a, p, blocks, rows, clear, u)) return;
   const int jt = (u.count + 15) / 16;
@@ -687,9 +710,10 @@ __global__ __launch_bounds__(256) void i8_combine(I8Args a) {
 }
 
 template <int DTYPE, int THREADS>
-void start_prepare(const TokenArgs& t, const I8Args& a, const Plan& p, int n_plan, bool skip, hipStream_t stream) {
+void start_prepare(const TokenArgs& t, const I8Args& a, const Plan& p, int n_plan, int skip, hipStream_t stream) {
   constexpr int kRows = THREADS / 64;
-  const dim3 grid(static_cast<uint32_t>(n_plan + std::min<int64_t>((t.rows + kRows - 1) / kRows, 1 << 20)));
+  const int per = std::max(skip, 1);
+  const dim3 grid(static_cast<uint32_t>(n_plan + std::min<int64_t>((t.rows + kRows * per - 1) / (kRows * per), 1 << 20)));
   auto* kernel = t.K <= kWaveChunk       ? i8_prepare<DTYPE, 1, THREADS>
                  : t.K <= 2 * kWaveChunk ? i8_prepare<DTYPE, 2, THREADS>
                  : t.K <= 4 * kWaveChunk ? i8_prepare<DTYPE, 4, THREADS>
@@ -700,12 +724,12 @@ void start_prepare(const TokenArgs& t, const I8Args& a, const Plan& p, int n_pla
 
 // Many pairs are looked through by more threads.
 template <int DTYPE>
-void start_prepare(const TokenArgs& t, const I8Args& a, const Plan& p, int n_plan, bool skip, hipStream_t stream) {
+void start_prepare(const TokenArgs& t, const I8Args& a, const Plan& p, int n_plan, int skip, hipStream_t stream) {
   if (n_plan > 0 && a.n_tokens * a.k > 8192) start_prepare<DTYPE, 1024>(t, a, p, n_plan, skip, stream);
   else start_prepare<DTYPE, 256>(t, a, p, n_plan, skip, stream);
 }
 
-void start_prepare(const TokenArgs& t, int32_t dtype, const I8Args& a, const Plan& p, int n_plan, bool skip, hipStream_t stream) {
+void start_prepare(const TokenArgs& t, int32_t dtype, const I8Args& a, const Plan& p, int n_plan, int skip, hipStream_t stream) {
   if (dtype == TACG_F32) start_prepare<TACG_F32>(t, a, p, n_plan, skip, stream);
   else if (dtype == TACG_BF16) start_prepare<TACG_BF16>(t, a, p, n_plan, skip, stream);
   else start_prepare<TACG_F16>(t, a, p, n_plan, skip, stream);
@@ -727,8 +751,8 @@ TokenArgs token_args(const void* x, int64_t stride_token, int64_t stride_slot, i
   return t;
 }
 
-// Whether so few pairs fall to a matrix, on average, that their time is that of the weights' loads.
-bool few_pairs(int64_t pairs, int32_t n_experts) { return pairs <= 24 * static_cast<int64_t>(n_experts); }
+// Pairs of a tile: whether so few fall to a matrix, on average, that their time is that of the weights' loads.
+int tile_of(int64_t pairs, int32_t n_experts) { return pairs <= 24 * static_cast<int64_t>(n_experts) ? kFewTile : kManyTile; }
 
 // The parts of a call's workspace.
 struct Space {
@@ -748,11 +772,11 @@ Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_experts, i
     s.levels = ws.take<int8_t>(rows * ((n_cols + kTileCols - 1) / kTileCols * kTileCols));
     s.scales = ws.take<float>(rows);
   }
-  s.plan.tile = few_pairs(pairs, n_experts) ? kFewTile : kManyTile;
+  s.plan.tile = tile_of(pairs, n_experts);
   s.plan.sparse = pairs <= n_held;
   s.plan.n_tiles = s.plan.sparse ? static_cast<int32_t>(pairs) : static_cast<int32_t>(pairs / s.plan.tile + n_held);
   s.plan.order = ws.take<int32_t>(pairs);
-  s.plan.first = ws.take<int32_t>(n_held + 2);
+  s.plan.first = ws.take<int32_t>(n_held + 1);
   s.plan.tiles = ws.take<int2>(s.plan.n_tiles);
   if (mode == TACG_Q4_SUM && top_k > 1) s.part = ws.take<float>(pairs * n_rows);
   s.bytes = ws.used;
@@ -782,7 +806,7 @@ int launch_i8_pack(const void* w, int32_t dtype, int64_t n_matrices, int32_t n_r
 
 int launch_token_i8(const void* x, int32_t dtype, int64_t row_stride, int64_t n_rows, int32_t n_cols, int8_t* q, float* scale,
                     uint32_t* d_err, hipStream_t stream) {
-  start_prepare(token_args(x, row_stride, 0, n_rows, 1, n_cols, q, scale, d_err), dtype, I8Args{}, Plan{}, 0, false, stream);
+  start_prepare(token_args(x, row_stride, 0, n_rows, 1, n_cols, q, scale, d_err), dtype, I8Args{}, Plan{}, 0, 0, stream);
   return hipGetLastError() == hipSuccess ? TACG_OK : TACG_E_DEVICE;
 }
 
@@ -830,16 +854,16 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
   const int width = mode == TACG_Q4_GLU ? n_rows / 2 : n_rows, per = frags * kTileRows / (mode == TACG_Q4_GLU ? 2 : 1);
   const int blocks = (width + per - 1) / per;
   if (ids == nullptr) s.plan.n_tiles = static_cast<int>((n_tokens + s.plan.tile - 1) / s.plan.tile) * n_held;
-  const int clear = ids != nullptr && s.part == nullptr ? static_cast<int>(std::min<int64_t>(n_tokens * top_k, 256)) : 0;
+  const int clear = ids != nullptr && s.part == nullptr ? static_cast<int>(std::min<int64_t>((n_tokens * top_k + 255) / 256, 512)) : 0;
   const int64_t grid = static_cast<int64_t>(s.plan.n_tiles) * blocks + clear;
   if (grid >= (int64_t(1) << 32) / 256) return TACG_E_UNSUPPORTED;  // threads that a launch holds; results of more than 288 GB
-  const int n_plan = ids != nullptr ? n_held + 1 : 0;
+  const int n_plan = ids != nullptr ? std::max(n_held, 1) : 0;
   if (dtype == TACG_I8) {
     a.x = static_cast<const int8_t*>(x);
     a.x_scale = x_scale;
     a.x_token = stride_token;
     a.x_slot = stride_slot;
-    if (n_plan > 0) start_prepare(TokenArgs{}, TACG_BF16, a, s.plan, n_plan, false, stream);
+    if (n_plan > 0) start_prepare(TokenArgs{}, TACG_BF16, a, s.plan, n_plan, 0, stream);
   } else {
     const int64_t width = static_cast<int64_t>(a.col_tiles) * kTileCols;
     const int64_t rows = n_tokens * (slots ? top_k : 1);
@@ -848,7 +872,8 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
     a.x_scale = s.scales;
     a.x_token = width * (slots ? top_k : 1);
     a.x_slot = slots ? width : 0;
-    start_prepare(t, dtype, a, s.plan, n_plan, slots && ids != nullptr, stream);
+    const int skip = slots && ids != nullptr ? static_cast<int>(std::min<int64_t>(rows / 8192 + 1, 64)) : 0;
+    start_prepare(t, dtype, a, s.plan, n_plan, skip, stream);
   }
   if (hipGetLastError() != hipSuccess) return TACG_E_DEVICE;
   if (grid > 0) {

@@ -348,6 +348,9 @@ int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_
   a.top_groups = top_groups;
   a.group_size = n_experts / n_groups;
   a.group_best = group_best;
+  const int chunk = 16 / dtype_size(dtype);
+  a.group_chunks = a.group_size % chunk == 0 ? a.group_size / chunk : 0;
+  a.group_lanes = n_groups <= 2 ? 4 : n_groups <= 4 ? 2 : 1;
   a.group_mul = (65536 + a.group_size - 1) / a.group_size;
   a.trace = trace;
   a.gate = gate;

@@ -17,6 +17,8 @@ struct RouteArgs {
   int32_t n_layers, E, k, F, rows;               // rows: of a workgroup's run
   int32_t softmax, renorm, vec;                  // vec: bytes that a load may take at a time
   int32_t groups, top_groups, group_size, group_best;
+  int32_t group_chunks;                          // 16-byte chunks of a group, 0 where a chunk may hold two groups' experts
+  int32_t group_lanes;                           // lanes of a row that share a group then
   uint32_t group_mul;                            // e * group_mul >> 16 = e / group_size
   float scale;
   const float* bias;                             // [L][E] or null
@@ -44,7 +46,14 @@ constexpr int kRouteThreads = 256;
 constexpr int kRouteWaves = kRouteThreads / 64;
 constexpr int kRowsPerPass = kRouteThreads / kRowLanes;
 constexpr float kNone = -INFINITY;
-constexpr float kNear = 0x1p-16f;               // scores that 32 bits may hold in another order are nearer than this, relatively
+
+// How near two values v = s + bias, or sums of two, may be for 32 bits to hold them in another order.  `bias` bounds their biases' magnitude, so
+// s <= |v| + bias.  A score is exp of a difference d <= 0, or nearly: the argument is off by |d| 2^-23, the exp and, for the softmax, the
+// sum of all of them by 2^-19 more, so s is off by s 2^-18 while s > 2^-11 (|d| < 8) and by s 2^-15 at least down to the smallest.
+__device__ __forceinline__ float near_by(float v, float bias) {
+  const float s = fabsf(v) + bias;
+  return 0x1p-17f * s + 0x1p-14f * fminf(s, 0x1p-11f) + FLT_MIN;
+}
 
 struct BackArgs {
   const void* logits;
@@ -259,6 +268,11 @@ __device__ __forceinline__ double entry_of(double v, int e) {  // the same of 64
   const uint64_t bits = __builtin_bit_cast(uint64_t, v + 0.0) & ~uint64_t(0xff);
   return __builtin_bit_cast(double, bits | static_cast<uint32_t>(v < 0.0 ? e : 255 - e));
 }
+__device__ __forceinline__ int id_of(double entry) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, entry);
+  const int low = static_cast<int>(bits & 0xff);
+  return bits >> 63 ? low : 255 - low;
+}
 struct Run {
   int family;
   int64_t first, last;  // tokens
@@ -310,7 +324,13 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
   __shared__ float mass[BAL ? kRouteWaves : 1][BAL ? TACG_MAX_EXPERTS : 1];
   __shared__ float squares[kRouteWaves];
   __shared__ uint32_t routed[kRouteWaves];
-  __shared__ double group_score[GROUPS ? kRowsPerPass : 1][GROUPS ? TACG_MAX_GROUPS + 1 : 1];
+  // GROUPS: the two largest values of each chunk of a row (rows in different banks, two by two), the groups' scores, and the chosen
+  // experts' values in order
+  constexpr int kPairs = CH * kRowLanes, kPairStride = (kPairs + 15) / 16 * 16 + 8;
+  __shared__ float2 two[GROUPS ? kRowsPerPass : 1][GROUPS ? kPairStride : 1];
+  __shared__ float group_score[GROUPS ? kRowsPerPass : 1][GROUPS ? TACG_MAX_GROUPS + 1 : 1];
+  __shared__ double group_score64[GROUPS ? kRowsPerPass : 1][GROUPS ? TACG_MAX_GROUPS + 1 : 1];
+  __shared__ float ranked[GROUPS && BIAS ? kRowsPerPass : 1][GROUPS && BIAS ? KL + 2 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & (kRowLanes - 1);
   const int l = blockIdx.y;
   const Run run = run_of(a, blockIdx.x);
@@ -375,47 +395,131 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
       return s;
     };
     auto allowed = [&](int e) { return (kept >> (((e * a.group_mul) >> 16) & 31)) & 1u; };
-    if constexpr (GROUPS) {
-      if (BIAS && a.softmax) {
-        double total = 0.0;
-        for (int e = sub; e < E; e += kRowLanes) total += exp(static_cast<double>(logit[e]) - static_cast<double>(from));
+    // the sum of all scores, in 64 bits: where a bias is added to them
+    auto total64 = [&] {
+      if (!BIAS || !a.softmax) return;
+      double sum = 0.0;
+      for (int e = sub; e < E; e += kRowLanes) sum += exp(static_cast<double>(logit[e]) - static_cast<double>(from));
 #pragma unroll
-        for (int o = 1; o < kRowLanes; o <<= 1) total += __shfl_xor(total, o, 64);
-        inverse64 = total > 0.0 ? 1.0 / total : 0.0;
-      }
-      double* score = group_score[tid >> 3];
-      for (int g = sub; g < a.groups; g += kRowLanes) {
-        double first = -INFINITY, second = -INFINITY;
-        for (int e = g * a.group_size; e < (g + 1) * a.group_size; ++e) {
-          if (!(logit[e] > kNone)) continue;
-          const double v = BIAS || a.group_best > 1 ? value64(logit[e], e) : static_cast<double>(logit[e]);
-          if (v > first) second = first, first = v;
-          else if (v > second) second = v;
+      for (int o = 1; o < kRowLanes; o <<= 1) sum += __shfl_xor(sum, o, 64);
+      inverse64 = sum > 0.0 ? 1.0 / sum : 0.0;
+    };
+    // the groups that are kept, of the values y (logits, or scores with a bias; -inf: not available)
+    auto keep_groups = [&](const float (&y)[M], float most_bias, auto value32) {
+      // the sum of a group's best values from the best logits; those of a bias are there
+      auto sum32 = [&](float first, float second) {
+        if (BIAS) return a.group_best > 1 && second > kNone ? first + second : first;
+        if (a.group_best == 1 || first == kNone) return first;
+        auto s = [&](float v) { return v == kNone ? 0.0f : a.softmax ? __expf(v - from) : sigmoid(v); };
+        return s(first) + s(second);
+      };
+      auto take = [&](float& first, float& second, float f, float s) {
+        second = vmax3(vmin(first, f), second, s);
+        first = vmax(first, f);
+      };
+      float* score = group_score[tid >> 3];
+      float2* pairs = two[tid >> 3];
+      if (a.group_chunks > 0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          float first = y[c * V], second = kNone;
+#pragma unroll
+          for (int i = 1; i < V; ++i) {
+            second = vmax(second, vmin(first, y[c * V + i]));
+            first = vmax(first, y[c * V + i]);
+          }
+          pairs[c * kRowLanes + sub] = make_float2(first, second);
         }
-        score[g] = a.group_best > 1 && second > -INFINITY ? first + second : first;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int n = a.group_chunks;
+        for (int g = sub; g < a.groups; g += kRowLanes) {
+          float first = kNone, second = kNone;
+          int i = sub % n;  // lanes start in different banks
+          for (int c = 0; c < n; ++c) {
+            const float2 v = pairs[g * n + i];
+            take(first, second, v.x, v.y);
+            i = i + 1 == n ? 0 : i + 1;
+          }
+          score[g] = sum32(first, second);
+        }
+      } else {
+        const int lanes = a.group_lanes, part = sub & (lanes - 1);
+        for (int g = lanes > 1 ? sub / lanes : sub; g < a.groups; g += kRowLanes) {
+          float first = kNone, second = kNone;
+          for (int e = g * a.group_size + part; e < (g + 1) * a.group_size; e += lanes)
+            if (logit[e] > kNone) take(first, second, value32(logit[e], e), kNone);
+          if (lanes > 1) take(first, second, across<kSwap1>(first), across<kSwap1>(second));
+          if (lanes > 2) take(first, second, across<kSwap2>(first), across<kSwap2>(second));
+          score[g] = sum32(first, second);
+        }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      kept = 0;
+      bool near = false;
+      const bool exact = !BIAS && a.group_best == 1;  // logits
       for (int g = sub; g < a.groups; g += kRowLanes) {
+        const float own = score[g], margin = near_by(own, 2.0f * most_bias);
         int better = 0;
-        for (int h = 0; h < a.groups; ++h) better += score[h] > score[g] || (score[h] == score[g] && h < g);
-        if (score[g] > -INFINITY && better < a.top_groups) kept |= 1u << g;
+        for (int h = 0; h < a.groups; ++h) {
+          const float d = score[h] - own;
+          better += score[h] > own || (score[h] == own && h < g);
+          near |= !exact && h != g && fabsf(d) <= margin;
+        }
+        if (own > kNone && better < a.top_groups) kept |= 1u << g;
+      }
+      if (__any(near)) {
+        total64();
+        double* score64 = group_score64[tid >> 3];
+        for (int g = sub; g < a.groups; g += kRowLanes) {
+          double first = -INFINITY, second = -INFINITY;
+          for (int e = g * a.group_size; e < (g + 1) * a.group_size; ++e) {
+            if (!(logit[e] > kNone)) continue;
+            const double v = value64(logit[e], e);
+            if (v > first) second = first, first = v;
+            else if (v > second) second = v;
+          }
+          score64[g] = a.group_best > 1 && second > -INFINITY ? first + second : first;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        kept = 0;
+        for (int g = sub; g < a.groups; g += kRowLanes) {
+          int better = 0;
+          for (int h = 0; h < a.groups; ++h) better += score64[h] > score64[g] || (score64[h] == score64[g] && h < g);
+          if (score64[g] > -INFINITY && better < a.top_groups) kept |= 1u << g;
+        }
       }
       kept |= across<kSwap1>(static_cast<int>(kept));
       kept |= across<kSwap2>(static_cast<int>(kept));
       kept |= across<kMirror>(static_cast<int>(kept));
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
+    };
+    // y without the experts of other groups
+    auto limit = [&](float (&y)[M]) {
+      if (a.group_chunks > 0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const bool in = allowed((c * kRowLanes + sub) * V);
+#pragma unroll
+          for (int i = 0; i < V; ++i) y[c * V + i] = in ? y[c * V + i] : kNone;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < M; ++i) y[i] = allowed(element<T, CH>(i, sub)) ? y[i] : kNone;
+      }
+    };
     if constexpr (GROUPS && !BIAS) {
+      keep_groups(x, 0.0f, [](float v, int) { return v; });
       float y[M], unused;
 #pragma unroll
-      for (int i = 0; i < M; ++i) y[i] = allowed(element<T, CH>(i, sub)) ? x[i] : kNone;
+      for (int i = 0; i < M; ++i) y[i] = x[i];
+      limit(y);
       bound = lower_bound<KL>(y, unused);
       mask = at_least(y, vmax(bound, -FLT_MAX));
     }
     if constexpr (!BIAS && !GROUPS) mask = at_least(x, vmax(bound, -FLT_MAX));
     // scores: exp(x - top) (softmax, to be divided by their sum) or the sigmoid, in place of the logits
     const float shift = some ? top : 0.0f;
-    float total = 0.0f, inverse = 0.0f;
+    float total = 0.0f, inverse = 0.0f, widest = 0.0f;
     if (all) {
       uint32_t away = 0;  // BIAS: which logits are -inf
       if constexpr (BIAS) away = ~at_least(x, -FLT_MAX);
@@ -439,25 +543,30 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
         for (int i = 0; i < M; ++i) {
           const int e = element<T, CH>(i, sub);
           const float b = a.bias[l * E + (e < E ? e : 0)];
-          if constexpr (GROUPS) {
-            if (!allowed(e)) away |= 1u << (M - 1 - i);
-            most_bias = fmaxf(most_bias, fabsf(b));
-          }
+          if constexpr (GROUPS) most_bias = fmaxf(most_bias, fabsf(b));
           x[i] = (away >> (M - 1 - i)) & 1u ? kNone : x[i] * f + b;
+        }
+        if constexpr (GROUPS) {
+          most_bias = row_max(most_bias);
+          keep_groups(x, most_bias, [&](float v, int e) { return (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e]; });
+          limit(x);
+          widest = most_bias;
         }
         float unused;
         bound = lower_bound<KL>(x, unused);
-        // a score of 32 bits may be off by 2^-17 of itself, and is at most the value and the largest bias
-        if constexpr (GROUPS) bound -= kNear * (fabsf(bound) + row_max(most_bias)) + FLT_MIN;
+        if constexpr (GROUPS) bound -= near_by(bound, most_bias);
         mask = at_least(x, vmax(bound, -FLT_MAX));
       }
     }
     // what the selection orders by, of one expert
     using Key = std::conditional_t<GROUPS && BIAS, double, float>;
     auto value = [&](float v, int e) {
+      if constexpr (BIAS) v = (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e];
+      return v;
+    };
+    auto order_by = [&](float v, int e) {
       if constexpr (GROUPS && BIAS) return value64(v, e);
-      else if constexpr (BIAS) v = (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e];
-      if constexpr (!(GROUPS && BIAS)) return v;
+      else return value(v, e);
     };
     // the list: each lane's elements after those of the lanes before it
     int n = __popc(mask), before = 0;
@@ -501,17 +610,18 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       // entries sub, sub + 8, ... of the lane; those past the end order behind all others
-      auto place = [&](auto entries) {
+      auto place = [&](auto entries, auto value_of) {
         constexpr int N = entries.value;
+        constexpr bool again = std::is_same_v<decltype(value_of(0.0f, 0)), double>;  // the ids are those of the entries before
         int e[N], larger[N];
         float x[N];
         double own[N];
 #pragma unroll
         for (int q = 0; q < N; ++q) {
           const bool have = sub + q * kRowLanes < n;
-          e[q] = have ? ids[sub + q * kRowLanes] : 0;
+          e[q] = !have ? 0 : again ? id_of(mine[sub + q * kRowLanes]) : ids[sub + q * kRowLanes];
           x[q] = logit[e[q]];
-          own[q] = have ? entry_of(value(x[q], e[q]), e[q]) : -INFINITY;
+          own[q] = have ? entry_of(value_of(x[q], e[q]), e[q]) : -INFINITY;
           larger[q] = 0;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -531,14 +641,36 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
 #pragma unroll
         for (int q = 0; q < N; ++q)
           if (sub + q * kRowLanes < n && larger[q] < k) slots[larger[q]] = make_float2(__int_as_float(e[q]), x[q]);
+        if constexpr (GROUPS && BIAS && !again) {
+#pragma unroll
+          for (int q = 0; q < N; ++q)
+            if (sub + q * kRowLanes < n && larger[q] <= k) ranked[tid >> 3][larger[q]] = static_cast<float>(own[q]);
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       };
-      if constexpr (KL == 16) {
-        if (most <= 3 * kRowLanes) place(std::integral_constant<int, 3>());
-        else place(std::integral_constant<int, 4>());
+      auto place_all = [&](auto value_of) {
+        if constexpr (KL == 16) {
+          if (most <= 3 * kRowLanes) place(std::integral_constant<int, 3>(), value_of);
+          else place(std::integral_constant<int, 4>(), value_of);
+        } else {
+          if (most <= kRowLanes) place(std::integral_constant<int, 1>(), value_of);
+          else place(std::integral_constant<int, 2>(), value_of);
+        }
+      };
+      if constexpr (GROUPS && BIAS) {
+        float* order = ranked[tid >> 3];
+        for (int j = sub; j <= k; j += kRowLanes) order[j] = kNone;
+        place_all(value);
+        // neighbours that 32 bits may hold in another order, the first that is not chosen among them
+        bool near = false;
+        for (int j = sub; j < k; j += kRowLanes)
+          near |= order[j + 1] > kNone && order[j] - order[j + 1] <= near_by(order[j], widest);
+        if (__any(near)) {
+          total64();
+          place_all(value64);
+        }
       } else {
-        if (most <= kRowLanes) place(std::integral_constant<int, 1>());
-        else place(std::integral_constant<int, 2>());
+        place_all(value);
       }
 #pragma unroll
       for (int q = 0; q < KS; ++q) {
@@ -549,6 +681,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     } else {
       // k passes: the best after the last winner in (value descending, id ascending)
+      if constexpr (GROUPS && BIAS) total64();
       Key last = INFINITY;
       int last_e = -1;
       for (int j = 0; j < k; ++j) {
@@ -557,7 +690,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
         for (int i = 0; i < M; ++i) {
           const int e = element<T, CH>(i, sub);
           if (e >= E || (GROUPS && !allowed(e))) continue;
-          const Key v = logit[e] > kNone ? value(logit[e], e) : static_cast<Key>(kNone);
+          const Key v = logit[e] > kNone ? order_by(logit[e], e) : static_cast<Key>(kNone);
           const bool after = v < last || (v == last && e > last_e);
           if (after && v > best) best = v, at = e;
         }

@@ -330,6 +330,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
   __shared__ float2 two[GROUPS ? kRowsPerPass : 1][GROUPS ? kPairStride : 1];
   __shared__ float group_score[GROUPS ? kRowsPerPass : 1][GROUPS ? TACG_MAX_GROUPS + 1 : 1];
   __shared__ double group_score64[GROUPS ? kRowsPerPass : 1][GROUPS ? TACG_MAX_GROUPS + 1 : 1];
+  __shared__ alignas(16) float bias_of[GROUPS && BIAS ? TACG_MAX_EXPERTS : 4];  // the layer's
   __shared__ float ranked[GROUPS && BIAS ? kRowsPerPass : 1][GROUPS && BIAS ? KL + 2 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & (kRowLanes - 1);
   const int l = blockIdx.y;
@@ -349,6 +350,14 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
     if (tid == 0 && run.start) a.arrived[static_cast<int64_t>(run.family) * a.n_layers + l] = 0;
     __syncthreads();
   }
+  if constexpr (GROUPS && BIAS) {
+    for (int e = tid; e < TACG_MAX_EXPERTS; e += kRouteThreads) bias_of[e] = e < E ? a.bias[l * E + e] : 0.0f;
+    __syncthreads();
+  }
+  auto bias_at = [&](int e) {
+    if constexpr (GROUPS) return bias_of[e];
+    else return a.bias[l * E + e];
+  };
   // whether the sum over all experts is needed
   const bool all = BAL || BIAS || a.norm != nullptr || (a.softmax && !a.renorm);
   for (int64_t base = run.first; base < run.last; base += kRowsPerPass) {
@@ -391,7 +400,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
     const float from = some ? top : 0.0f;
     auto value64 = [&](float v, int e) {
       double s = a.softmax ? exp(static_cast<double>(v) - static_cast<double>(from)) * inverse64 : 1.0 / (1.0 + exp(-static_cast<double>(v)));
-      if constexpr (BIAS) s += static_cast<double>(a.bias[l * E + e]);
+      if constexpr (BIAS) s += static_cast<double>(bias_of[e]);
       return s;
     };
     auto allowed = [&](int e) { return (kept >> (((e * a.group_mul) >> 16) & 31)) & 1u; };
@@ -542,13 +551,13 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
 #pragma unroll
         for (int i = 0; i < M; ++i) {
           const int e = element<T, CH>(i, sub);
-          const float b = a.bias[l * E + (e < E ? e : 0)];
+          const float b = bias_at(GROUPS ? e : e < E ? e : 0);
           if constexpr (GROUPS) most_bias = fmaxf(most_bias, fabsf(b));
           x[i] = (away >> (M - 1 - i)) & 1u ? kNone : x[i] * f + b;
         }
         if constexpr (GROUPS) {
           most_bias = row_max(most_bias);
-          keep_groups(x, most_bias, [&](float v, int e) { return (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e]; });
+          keep_groups(x, most_bias, [&](float v, int e) { return (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + bias_of[e]; });
           limit(x);
           widest = most_bias;
         }
@@ -561,7 +570,7 @@ __global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
     // what the selection orders by, of one expert
     using Key = std::conditional_t<GROUPS && BIAS, double, float>;
     auto value = [&](float v, int e) {
-      if constexpr (BIAS) v = (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e];
+      if constexpr (BIAS) v = (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + bias_at(e);
       return v;
     };
     auto order_by = [&](float v, int e) {

@@ -32,6 +32,302 @@
 
 namespace tacg {
 namespace {
+// grid: (runs, layers).  KL: the smallest of 4, 8 and 16 that is not below k.
+template <class T, int CH, int KL, bool BAL, bool BIAS>
+__global__ __launch_bounds__(kRouteThreads, 2) void route_main(RouteArgs a) {
+  constexpr int V = kChunk<T>, M = CH * V, KS = (KL + kRowLanes - 1) / kRowLanes;
+  constexpr int kList = KL < 8 ? 16 : 2 * KL;  // elements of a row's list
+  __shared__ double list[kRowsPerPass][kList];
+  __shared__ alignas(16) float copy[kRowsPerPass][M * kRowLanes + 4];  // the rows' logits: rows in different banks
+  __shared__ float2 chosen[kRowsPerPass][KS * kRowLanes];
+  __shared__ uint32_t count[BAL ? TACG_MAX_EXPERTS : 1];
+  __shared__ float mass[BAL ? kRouteWaves : 1][BAL ? TACG_MAX_EXPERTS : 1];
+  __shared__ float squares[kRouteWaves];
+  __shared__ uint32_t routed[kRouteWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & (kRowLanes - 1);
+  const int l = blockIdx.y;
+  const Run run = run_of(a, blockIdx.x);
+  const int E = a.E, k = a.k;
+  const T* layer = static_cast<const T*>(a.logits) + l * a.stride_layer;
+  double* mine = list[tid >> 3];
+  float2* slots = chosen[tid >> 3];
+  float* logit = copy[tid >> 3];
+  float acc[BAL ? M : 1];
+  float sq = 0.0f;
+  uint32_t live = 0;
+  if (BAL) {
+#pragma unroll
+    for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] = 0.0f;
+    for (int e = tid; e < E; e += kRouteThreads) count[e] = 0;
+    if (tid == 0 && run.start) a.arrived[static_cast<int64_t>(run.family) * a.n_layers + l] = 0;
+    __syncthreads();
+  }
+  // whether the sum over all experts is needed
+  const bool all = BAL || BIAS || a.norm != nullptr || (a.softmax && !a.renorm);
+  for (int64_t base = run.first; base < run.last; base += kRowsPerPass) {
+    const int64_t t = base + (tid >> 3);
+    const bool in = t < run.last;
+    const T* row = layer + (in ? t : run.first) * a.stride_token;
+    float x[M];
+    load_row<T, CH>(row, sub, E, a.vec, x);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < M; i += 2) bad |= __builtin_isunordered(x[i], x[i + 1]);
+    float top, bound = 0.0f;
+    if constexpr (BIAS) {
+      top = x[0];
+#pragma unroll
+      for (int i = 1; i < M; ++i) top = vmax(top, x[i]);
+      top = row_max(top);
+    } else {
+      bound = lower_bound<KL>(x, top);
+    }
+    bad |= top == INFINITY;
+    if (__any(bad)) {  // a NaN or +inf: the row is not routed
+      const uint64_t m = __ballot(bad) >> (lane & ~(kRowLanes - 1));
+      if ((m & 0xff) != 0) {
+        if (in && sub == 0) atomicOr(a.err, TACG_ERR_VALUE);
+        top = bound = kNone;
+#pragma unroll
+        for (int i = 0; i < M; ++i) x[i] = kNone;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < M; i += 4)
+      *reinterpret_cast<float4*>(logit + element<T, CH>(i, sub)) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const bool some = top > kNone;
+    uint32_t mask = 0;
+    if constexpr (!BIAS) mask = at_least(x, vmax(bound, -FLT_MAX));
+    // scores: exp(x - top) (softmax, to be divided by their sum) or the sigmoid, in place of the logits
+    const float shift = some ? top : 0.0f;
+    float total = 0.0f, inverse = 0.0f;
+    if (all) {
+      uint32_t away = 0;  // BIAS: which logits are -inf
+      if constexpr (BIAS) away = ~at_least(x, -FLT_MAX);
+      if (a.softmax) {
+#pragma unroll
+        for (int i = 0; i < M; ++i) x[i] = __expf(x[i] - shift), total += x[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < M; ++i) x[i] = sigmoid(x[i]), total += x[i];
+      }
+      total = row_sum(total);
+      inverse = total > 0.0f ? 1.0f / total : 0.0f;
+      if (BAL && in) {
+#pragma unroll
+        for (int i = 0; i < (BAL ? M : 1); ++i) acc[i] += x[i] * inverse;
+      }
+      if constexpr (BIAS) {
+        const float f = a.softmax ? inverse : 1.0f;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+          const int e = element<T, CH>(i, sub);
+          x[i] = (away >> (M - 1 - i)) & 1u ? kNone : x[i] * f + a.bias[l * E + (e < E ? e : 0)];
+        }
+        float unused;
+        bound = lower_bound<KL>(x, unused);
+        mask = at_least(x, vmax(bound, -FLT_MAX));
+      }
+    }
+    // what the selection orders by, of one expert
+    auto value = [&](float v, int e) {
+      if constexpr (BIAS) v = (a.softmax ? __expf(v - shift) * inverse : sigmoid(v)) + a.bias[l * E + e];
+      return v;
+    };
+    // the list: each lane's elements after those of the lanes before it
+    int n = __popc(mask), before = 0;
+    {
+      int o = across<kSwap1>(n);
+      before += sub & 1 ? o : 0;
+      n += o;
+      o = across<kSwap2>(n);
+      before += sub & 2 ? o : 0;
+      n += o;
+      o = across<kMirror>(n);
+      before += sub & 4 ? o : 0;
+      n += o;
+    }
+    int most = 0;  // of the wave's rows
+#pragma unroll
+    for (int r = 0; r < 64; r += kRowLanes) {
+      const int v = __builtin_amdgcn_readlane(n, r);
+      most = v > most ? v : most;
+    }
+    int id[KS];   // of slots sub, sub + 8: expert and its logit
+    float w[KS];
+#pragma unroll
+    for (int q = 0; q < KS; ++q) id[q] = -1, w[q] = kNone;
+    if (most <= kList) {
+      int32_t* ids = reinterpret_cast<int32_t*>(mine);  // before the entries
+#pragma unroll
+      for (int q = 0; q < KS; ++q) slots[sub + q * kRowLanes] = make_float2(__int_as_float(-1), kNone);
+      if constexpr (M <= 8) {
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+          if ((mask >> (M - 1 - i)) & 1u) ids[before++] = element<T, CH>(i, sub);
+      } else {
+        while (__any(mask != 0)) {
+          if (mask != 0) {
+            const int i = __clz(mask) - (32 - M);
+            mask &= ~(1u << (M - 1 - i));
+            ids[before++] = element<T, CH>(i, sub);
+          }
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      // entries sub, sub + 8, ... of the lane; those past the end order behind all others
+      auto place = [&](auto entries) {
+        constexpr int N = entries.value;
+        int e[N], larger[N];
+        float x[N];
+        double own[N];
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+          const bool have = sub + q * kRowLanes < n;
+          e[q] = have ? ids[sub + q * kRowLanes] : 0;
+          x[q] = logit[e[q]];
+          own[q] = have ? entry_of(value(x[q], e[q]), e[q]) : -INFINITY;
+          larger[q] = 0;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int q = 0; q < N; ++q) mine[sub + q * kRowLanes] = own[q];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int first = 0; first < N * kRowLanes; first += kRowLanes) {
+          double other[kRowLanes];
+#pragma unroll
+          for (int i = 0; i < kRowLanes; ++i) other[i] = mine[first + i];
+#pragma unroll
+          for (int i = 0; i < kRowLanes; ++i)
+#pragma unroll
+            for (int q = 0; q < N; ++q) larger[q] += other[i] > own[q];
+        }
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+          if (sub + q * kRowLanes < n && larger[q] < k) slots[larger[q]] = make_float2(__int_as_float(e[q]), x[q]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      };
+      if constexpr (KL == 16) {
+        if (most <= 3 * kRowLanes) place(std::integral_constant<int, 3>());
+        else place(std::integral_constant<int, 4>());
+      } else {
+        if (most <= kRowLanes) place(std::integral_constant<int, 1>());
+        else place(std::integral_constant<int, 2>());
+      }
+#pragma unroll
+      for (int q = 0; q < KS; ++q) {
+        const float2 v = slots[sub + q * kRowLanes];
+        id[q] = __float_as_int(v.x);
+        w[q] = v.y;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    } else {
+      // k passes: the best after the last winner in (value descending, id ascending)
+      float last = INFINITY;
+      int last_e = -1;
+      for (int j = 0; j < k; ++j) {
+        float best = kNone;
+        int at = 0x7fffffff;
+        for (int i = 0; i < M; ++i) {
+          const int e = element<T, CH>(i, sub);
+          if (e >= E) continue;
+          const float v = logit[e] > kNone ? value(logit[e], e) : kNone;
+          const bool after = v < last || (v == last && e > last_e);
+          if (after && v > best) best = v, at = e;
+        }
+#pragma unroll
+        for (int o = 1; o < kRowLanes; o <<= 1) {
+          const float v = __shfl_xor(best, o, 64);
+          const int e = __shfl_xor(at, o, 64);
+          if (v > best || (v == best && e < at)) best = v, at = e;
+        }
+#pragma unroll
+        for (int q = 0; q < KS; ++q)
+          if (j == sub + q * kRowLanes && best > kNone) id[q] = at, w[q] = logit[at];
+        last = best;
+        last_e = best > kNone ? at : 0x7fffffff;
+      }
+    }
+    // gates of the selected
+    if (a.softmax) {
+      float high = shift;
+      if (BIAS && a.renorm) {
+        high = kNone;
+#pragma unroll
+        for (int q = 0; q < KS; ++q) high = vmax(high, w[q]);
+        high = row_max(high);
+        high = high == kNone ? 0.0f : high;
+      }
+#pragma unroll
+      for (int q = 0; q < KS; ++q) w[q] = __expf(w[q] - high);
+    } else {
+#pragma unroll
+      for (int q = 0; q < KS; ++q) w[q] = sigmoid(w[q]);
+    }
+    float factor = 1.0f;
+    if (a.renorm) {
+      float part = 0.0f;
+#pragma unroll
+      for (int q = 0; q < KS; ++q) part += w[q];
+      part = row_sum(part);
+      factor = part > 0.0f ? 1.0f / part : 0.0f;
+    } else if (a.softmax) {
+      factor = inverse;
+    }
+    const int64_t at = static_cast<int64_t>(l) * a.n_tokens + t;
+    if (in) {
+#pragma unroll
+      for (int q = 0; q < KS; ++q) {
+        const int j = sub + q * kRowLanes;
+        if (j < k) {
+          a.trace[at * k + j] = static_cast<int16_t>(id[q]);
+          a.gate[at * k + j] = w[q] * factor * a.scale;  // the share first: factor * scale may be more than 32 bits hold
+          if (BAL && id[q] >= 0) atomicAdd(&count[id[q]], 1u);
+        }
+      }
+    }
+    if (all) {
+      const float norm = a.softmax ? (some ? top + __logf(total) : kNone) : total;
+      if (a.norm != nullptr && in && sub == 0) a.norm[at] = norm;
+      if (BAL && in && some && sub == 0) {
+        live += 1;
+        if (a.softmax) sq += norm * norm;
+      }
+    }
+  }
+  if (!BAL) return;
+  // the run's sums: rows of a wave, then the waves in order
+#pragma unroll
+  for (int i = 0; i < (BAL ? M : 1); ++i) {
+    acc[i] = rows_sum(acc[i]);
+    const int e = element<T, CH>(i, sub);
+    if (lane < kRowLanes && e < E) mass[wave][e] = acc[i];
+  }
+  sq = rows_sum(sq);
+#pragma unroll
+  for (int o = kRowLanes; o < 64; o <<= 1) live += __shfl_xor(live, o, 64);
+  if (lane == 0) squares[wave] = sq, routed[wave] = live;
+  barrier_after_lds_atomics();
+  const int64_t slot = static_cast<int64_t>(l) * gridDim.x + blockIdx.x;
+  for (int e = tid; e < E; e += kRouteThreads) {
+    float m = mass[0][e];
+#pragma unroll
+    for (int w = 1; w < (BAL ? kRouteWaves : 1); ++w) m += mass[w][e];
+    a.mass[slot * E + e] = m;
+    a.count[slot * E + e] = count[e];
+  }
+  if (tid == 0) {
+    double s = 0.0;
+    uint32_t n = 0;
+#pragma unroll
+    for (int w = 0; w < kRouteWaves; ++w) s += squares[w], n += routed[w];
+    a.squares[slot] = s;
+    a.routed[slot] = n;
+  }
+}
+
 struct ReduceArgs {
   const float* mass;
   const uint32_t* count;
@@ -299,6 +595,31 @@ int fill_runs(Args& a, const int64_t* fam_off_host, int32_t n_fam, int rows) {
   return static_cast<int>(runs);
 }
 
+template <class T, int CH, int KL>
+void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
+  auto* kernel = a.bias != nullptr ? (bal ? route_main<T, CH, KL, true, true> : route_main<T, CH, KL, false, true>)
+                                   : (bal ? route_main<T, CH, KL, true, false> : route_main<T, CH, KL, false, false>);
+  kernel<<<grid, kRouteThreads, 0, s>>>(a);
+}
+
+template <class T, int CH>
+void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
+  if (a.k <= 4) start_main<T, CH, 4>(a, bal, grid, s);
+  else if (a.k <= 8) start_main<T, CH, 8>(a, bal, grid, s);
+  else start_main<T, CH, 16>(a, bal, grid, s);
+}
+
+template <class T>
+void start_main(const RouteArgs& a, bool bal, dim3 grid, hipStream_t s) {
+  const int chunks = (a.E + kChunk<T> * kRowLanes - 1) / (kChunk<T> * kRowLanes);
+  if constexpr (sizeof(T) == 2) {
+    if (chunks <= 1) return start_main<T, 1>(a, bal, grid, s);
+  }
+  if (chunks <= 2) return start_main<T, 2>(a, bal, grid, s);
+  if (chunks <= 4) return start_main<T, 4>(a, bal, grid, s);
+  if constexpr (sizeof(T) == 4) start_main<T, 8>(a, bal, grid, s);
+}
+
 template <class T, int CH>
 void start_back(const BackArgs& a, dim3 grid, hipStream_t s) {
   auto* kernel = a.k > kRowLanes ? route_back<T, CH, 2> : route_back<T, CH, 1>;
@@ -349,7 +670,7 @@ int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_
   a.group_size = n_experts / n_groups;
   a.group_best = group_best;
   const int chunk = 16 / dtype_size(dtype);
-  a.group_chunks = a.group_size % chunk == 0 ? a.group_size / chunk : 0;
+  a.group_pairs = a.group_size % (2 * chunk) == 0 ? a.group_size / (2 * chunk) : 0;
   a.group_lanes = n_groups <= 2 ? 4 : n_groups <= 4 ? 2 : 1;
   a.group_mul = (65536 + a.group_size - 1) / a.group_size;
   a.trace = trace;
@@ -372,7 +693,9 @@ int launch_route(const void* logits, int32_t dtype, int64_t stride_layer, int64_
   if (runs > 0) {
     const dim3 grid(runs, n_layers);
     if (a.groups > 1) start_route_groups(a, dtype, bal, grid, stream);
-    else start_rows<false>(a, dtype, bal, grid, stream);
+    else if (dtype == TACG_F32) start_main<float>(a, bal, grid, stream);
+    else if (dtype == TACG_BF16) start_main<Bf16>(a, bal, grid, stream);
+    else start_main<F16>(a, bal, grid, stream);
     if (hipGetLastError() != hipSuccess) return TACG_E_DEVICE;
   }
   if (bal) {

@@ -183,7 +183,7 @@ __device__ void exact_row(const RouteArgs& a, const T* row, const float* bias, i
 
 // grid: (runs, layers).  KL: the smallest of 4, 8 and 16 that is not below k.
 template <class T, int CH, int KL, bool BAL, bool BIAS>
-__global__ __launch_bounds__(kRouteThreads, BAL ? 2 : 3) void route_grouped(RouteArgs a) {
+__global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
   constexpr int V = kChunk<T>, M = CH * V, KS = (KL + kRowLanes - 1) / kRowLanes;
   constexpr int kList = KL < 8 ? 16 : 2 * KL;  // elements of a row's list
   constexpr int kPairs = CH * kRowLanes / 2, kPairStride = (kPairs + 15) / 16 * 16 + 8;
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(kRouteThreads, BAL ? 2 : 3) void route_grouped(Rout
   };
   __shared__ Row rows[kRowsPerPass];
   __shared__ alignas(16) float copy[kRowsPerPass][M * kRowLanes + 4];  // the rows' logits: rows in different banks
-  __shared__ float group_score[kRowsPerPass][TACG_MAX_GROUPS + 1];
+  __shared__ alignas(16) float group_score[kRowsPerPass][TACG_MAX_GROUPS + 4];
   __shared__ alignas(16) float bias_of[BIAS ? TACG_MAX_EXPERTS : 4];   // the layer's
   __shared__ uint16_t hard_rows[kRunRows];                             // left for the end
   __shared__ int n_hard;
@@ -238,12 +238,14 @@ __global__ __launch_bounds__(kRouteThreads, BAL ? 2 : 3) void route_grouped(Rout
   __syncthreads();
   // whether the sum over all experts is needed
   const bool all = BAL || BIAS || a.norm != nullptr || (a.softmax && !a.renorm);
+  const bool whole = a.vec == 16 && E == M * kRowLanes;  // no lane has less than all its chunks
   for (int64_t base = run.first; base < run.last; base += kRowsPerPass) {
     const int64_t t = base + (tid >> 3);
     const bool in = t < run.last;
     const T* row = layer + (in ? t : run.first) * a.stride_token;
     float x[M];
-    load_row<T, CH>(row, sub, E, a.vec, x);
+    if (whole) load_row<T, CH>(row, sub, M * kRowLanes, 16, x);
+    else load_row<T, CH>(row, sub, E, a.vec, x);
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < M; i += 2) bad |= __builtin_isunordered(x[i], x[i + 1]);
@@ -270,10 +272,12 @@ __global__ __launch_bounds__(kRouteThreads, BAL ? 2 : 3) void route_grouped(Rout
     float total = 0.0f, inverse = 0.0f;
     // without a bias the logits order; scores are of their own
     auto scores = [&](float (&s)[M]) {
+      if (a.softmax) {
 #pragma unroll
-      for (int i = 0; i < M; ++i) {
-        s[i] = a.softmax ? __expf(x[i] - shift) : sigmoid(x[i]);
-        total += s[i];
+        for (int i = 0; i < M; ++i) s[i] = __expf(x[i] - shift), total += s[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < M; ++i) s[i] = sigmoid(x[i]), total += s[i];
       }
       total = row_sum(total);
       inverse = total > 0.0f ? 1.0f / total : 0.0f;
@@ -313,6 +317,7 @@ __global__ __launch_bounds__(kRouteThreads, BAL ? 2 : 3) void route_grouped(Rout
       };
       float* score = group_score[tid >> 3];
       float2* pairs = rows[tid >> 3].two;
+      for (int g = a.groups + sub; g < ((a.groups + 7) & ~7); g += kRowLanes) score[g] = kNone;
       auto keep = [&](int g, float first, float second) {
         if constexpr (BIAS) {
           score[g] = a.group_best > 1 && second > kNone ? first + second : first;
@@ -334,12 +339,15 @@ __global__ __launch_bounds__(kRouteThreads, BAL ? 2 : 3) void route_grouped(Rout
         const int n = a.group_pairs;
         for (int g = sub; g < a.groups; g += kRowLanes) {
           float first = kNone, second = kNone;
-          int i = sub & 3;  // lanes start in different banks
-          i = i < n ? i : 0;
-          for (int c = 0; c < n; ++c) {
-            const float2 v = pairs[g * n + i];
-            take(first, second, v.x, v.y);
-            i = i + 1 == n ? 0 : i + 1;
+          for (int c = 0; c < n; c += 4) {
+            float2 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int at = c + (n % 4 == 0 ? (i + sub) & 3 : i);  // lanes start in different banks
+              v[i] = at < n ? pairs[g * n + at] : make_float2(kNone, kNone);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) take(first, second, v[i].x, v[i].y);
           }
           keep(g, first, second);
         }
@@ -359,7 +367,13 @@ __global__ __launch_bounds__(kRouteThreads, BAL ? 2 : 3) void route_grouped(Rout
       for (int g = sub; g < a.groups; g += kRowLanes) {
         const float own = score[g];
         int better = 0;
-        for (int h = 0; h < a.groups; ++h) better += score[h] > own || (score[h] == own && h < g);
+        for (int h = 0; h < a.groups; h += 8) {  // those past the last are -inf
+          float s[8];
+          *reinterpret_cast<float4*>(s) = *reinterpret_cast<const float4*>(score + h);
+          *reinterpret_cast<float4*>(s + 4) = *reinterpret_cast<const float4*>(score + h + 4);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) better += s[i] > own || (s[i] == own && h + i < g);
+        }
         if (own > kNone && better < a.top_groups) kept |= 1u << g;
         const int at = better - a.top_groups + 1;
         if (at == 0 || at == 1) border[at] = own;

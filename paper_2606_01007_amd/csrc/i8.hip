@@ -23,10 +23,11 @@ constexpr int kTileRows = 16, kTileCols = 64, kTileBytes = kTileRows * kTileCols
 
 struct I8Args {
   const int8_t* x;          // levels
+  const void* tokens;       // few pairs: x as the caller has it, and its strides in elements
   const float* x_scale;
   int64_t x_token, x_slot;  // strides of the levels, in bytes
   int64_t n_tokens;
-  int32_t k, E, H, N, row_tiles, col_tiles, mode, out_dtype, slots;  // slots: whether every slot has its own x
+  int32_t k, E, H, N, K, row_tiles, col_tiles, mode, out_dtype, slots;  // slots: whether every slot has its own x
   uint32_t over_k;          // the high half of pair * over_k is pair / k (0 for k = 1): pairs are below 2^27, k up to 16
   const int16_t* ids;       // or null: slot j takes matrix j
   const int32_t* slot;      // [E] or null
@@ -402,8 +403,9 @@ __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f)
 }
 
 // Results of a wave: lane n + 16 q holds rows 4 q .. 4 q + 3 of a block for token n.
-template <int RF, int JT>
-__device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Unit& u, int n0, const int4v (&acc)[RF][JT]) {
+// pair_at(i): the pair of the tile's token i; scale_at(i, pair): the scale of its levels.
+template <int RF, int JT, class Pair, class Scale>
+__device__ __forceinline__ void finish(const I8Args& a, const Unit& u, int n0, const int4v (&acc)[RF][JT], Pair pair_at, Scale scale_at) {
   const int lane = threadIdx.x & 63;
   const bool glu = a.mode == TACG_Q4_GLU;
   const int width = glu ? a.N / 2 : a.N;
@@ -425,8 +427,8 @@ __device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Uni
     constexpr int j = decltype(block)::value;
     const int i0 = j * 16 + (lane & 15);
     if (i0 >= u.count) return;
-    const int pair = pair_of(a, p, u, i0);
-    const float sx = a.x_scale[a.slots ? pair : token_index(a, pair)];
+    const int pair = pair_at(i0);
+    const float sx = scale_at(i0, pair);
     const float gate = a.mode == TACG_Q4_SUM && !part && a.gate != nullptr ? a.gate[pair] : 1.0f;
     if (glu) {
       if constexpr (RF > 1) {
@@ -454,6 +456,12 @@ __device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Uni
       }
     }
   });
+}
+
+template <int RF, int JT>
+__device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Unit& u, int n0, const int4v (&acc)[RF][JT]) {
+  finish(a, u, n0, acc, [&](int i) { return pair_of(a, p, u, i); },
+         [&](int, int pair) { return a.x_scale[a.slots ? pair : token_index(a, pair)]; });
 }
 
 // Many tokens: a wave has 64 weight rows and all tokens of the tile, JT blocks of 16.  Steps of 64 columns: weights go from memory to the
@@ -683,6 +691,222 @@ __global__ __launch_bounds__(256, 2) void i8_stream(I8Args a, Plan p, int blocks
   else stream_product<RF, 1, SPLIT>(a, p, u, lds);
 }
 
+// ---- few pairs: one launch ---------------------------------------------------------------------
+//
+// Every workgroup looks at all pairs (up to 64, a lane each) and rounds the tokens that it needs by itself, into LDS: no launch before it.
+
+constexpr int kFewPairs = 64;
+
+// A row of x, in the caller's type, as levels in LDS (col_tiles * 64 bytes) by LANES lanes of which this is number i; 256: the workgroup.
+// The scale comes back.
+template <int DTYPE, int LANES>
+__device__ __forceinline__ float round_to_lds(const I8Args& a, int64_t first, int64_t scale_at, char* to, uint32_t* most, int i, bool report) {
+  const int width = a.col_tiles * kTileCols;
+  if constexpr (DTYPE == TACG_I8) {
+    for (int c = i * 16; c < width; c += LANES * 16) *reinterpret_cast<int4v*>(to + c) = load16(static_cast<const int8_t*>(a.tokens) + first + c);
+    return a.x_scale[scale_at];
+  } else {
+    constexpr int kStep = LANES * kChunk;
+    float kept[2][kChunk], v[kChunk];
+    uint32_t m = 0;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) load_chunk<DTYPE>(a.tokens, first, s * kStep + i * kChunk, a.K, kept[s]);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) m = largest(kept[s], m);
+    for (int c = 2 * kStep + i * kChunk; c < a.K; c += kStep) {
+      load_chunk<DTYPE>(a.tokens, first, c, a.K, v);
+      m = largest(v, m);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o, 64)));
+    if constexpr (LANES > 64) {
+      if ((i & 63) == 0) most[i >> 6] = m;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < LANES / 64; ++w) m = max(m, most[w]);
+      __syncthreads();
+    }
+    const bool bad = m >= 0x7f800000u;
+    const Rounder level(bad ? 0.0f : __uint_as_float(m));
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      if (s * kStep + i * kChunk < width) *reinterpret_cast<uint2*>(to + s * kStep + i * kChunk) = levels_of(level, kept[s], bad);
+    for (int c = 2 * kStep + i * kChunk; c < width; c += kStep) {
+      load_chunk<DTYPE>(a.tokens, first, c, a.K, v);
+      *reinterpret_cast<uint2*>(to + c) = levels_of(level, v, bad);
+    }
+    if (bad && report && i == 0) atomicOr(a.err, TACG_ERR_VALUE);
+    return bad ? NAN : __uint_as_float(m) / 127.0f;
+  }
+}
+
+// The lane's pair, of up to 64: where its matrix lies.  The first workgroup along the rows reports what is invalid.
+__device__ __forceinline__ int lane_place(const I8Args& a, bool report) {
+  const int lane = threadIdx.x & 63, pairs = static_cast<int>(a.n_tokens) * a.k;
+  int h = -1;
+  if (lane < pairs) h = place_of(a, lane, lane - token_index(a, lane) * a.k);
+  if (report && threadIdx.x < 64 && h < -1) atomicOr(a.err, h == kBadId ? TACG_ERR_ID_RANGE : TACG_ERR_TABLE);
+  return h;
+}
+
+// Each and gated products: grid (blocks of 32 weight rows, pairs).  The workgroup of the first pair of a matrix takes all its pairs; its four
+// waves have a quarter of the columns each.  lds: rows of levels, `stride` bytes apart.
+template <int DTYPE>
+__global__ __launch_bounds__(256, 2) void i8_few(I8Args a, int rows, int stride) {
+  constexpr int RF = 2, DEPTH = 4;
+  extern __shared__ char levels[];
+  __shared__ int4v sums[(kWaves - 1) * RF * 64];
+  __shared__ int list[kFewPairs];
+  __shared__ float scales[kFewPairs];
+  __shared__ uint32_t most[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool glu = a.mode == TACG_Q4_GLU;
+  const int width = glu ? a.N / 2 : a.N;
+  const int place = lane_place(a, blockIdx.x == 0 && blockIdx.y == 0);
+  Unit u;
+  u.n0 = blockIdx.x * rows;
+  u.h = __builtin_amdgcn_readlane(place, blockIdx.y);
+  u.first = 0;
+  if (u.h < 0) {
+    for (int n = u.n0 + tid; n < min(u.n0 + rows, width); n += 256) store(a.out, static_cast<int64_t>(blockIdx.y) * width + n, 0.0f, a.out_dtype);
+    return;
+  }
+  const uint64_t same = __ballot(place == u.h);
+  if ((same & ((uint64_t(1) << blockIdx.y) - 1)) != 0) return;
+  u.count = __popcll(same);
+  if (place == u.h && wave == 0) list[__popcll(same & ((uint64_t(1) << lane) - 1))] = lane;
+  const char* w = matrix_of(a, u.h);
+  uint32_t at[RF];
+  weight_rows<RF>(a, u.n0, glu, width, at);
+  const int begin = a.col_tiles * wave / kWaves, end = a.col_tiles * (wave + 1) / kWaves, last = max(end - 1, 0);
+  int4v v[DEPTH][RF];
+  auto load = [&](int c, int d) {
+#pragma unroll
+    for (int i = 0; i < RF; ++i) v[d][i] = load16(w + (at[i] + static_cast<uint32_t>(c) * kTileBytes));
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) load(min(begin + d, last), d);  // before the tokens are there
+  __syncthreads();
+  // 16 tokens at a time
+  for (int first = 0; first < u.count; first += 16) {
+    const int n = min(u.count - first, 16);
+    for (int r = 0; r < n; ++r) {
+      const int pair = list[first + r], t = token_index(a, pair);
+      const float s = round_to_lds<DTYPE, 256>(a, t * a.x_token + (pair - t * a.k) * a.x_slot, a.slots ? pair : t, levels + r * stride, most,
+                                               tid, blockIdx.x == 0);
+      if (tid == 0) scales[r] = s;
+    }
+    __syncthreads();
+    const char* token = levels + min(lane & 15, n - 1) * stride + (lane >> 4) * kPiece;
+    int4v acc[RF][1] = {};
+    auto multiply = [&](int c, int d) {
+      const int4v t = load16(token + c * kTileCols);
+#pragma unroll
+      for (int i = 0; i < RF; ++i) acc[i][0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[d][i], t, acc[i][0], 0, 0, 0);
+    };
+    if (first > 0) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) load(min(begin + d, last), d);
+    }
+    int c = begin;
+    for (; c + 2 * DEPTH <= end; c += DEPTH) {
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        multiply(c + d, d);
+        load(c + d + DEPTH, d);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+      if (c + d < end) {
+        multiply(c + d, d);
+        if (c + d + DEPTH < end) load(c + d + DEPTH, d);
+      }
+    c += DEPTH;
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+      if (c + d < end) multiply(c + d, d);
+    if (wave > 0) {
+#pragma unroll
+      for (int i = 0; i < RF; ++i) sums[((wave - 1) * RF + i) * 64 + lane] = acc[i][0];
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int o = 0; o < kWaves - 1; ++o)
+#pragma unroll
+        for (int i = 0; i < RF; ++i) acc[i][0] += sums[(o * RF + i) * 64 + lane];
+      Unit part = u;
+      part.count = n;
+      finish(a, part, u.n0, acc, [&](int i) { return list[first + i]; }, [&](int i, int) { return scales[i]; });
+    }
+    __syncthreads();
+  }
+}
+
+// Sums over a token's experts: grid (blocks of 16 weight rows, tokens), eight waves.  A wave rounds the x of one slot after another; then the
+// steps of all served slots are shared evenly, and a slot's (exact) sums meet in LDS.
+template <int DTYPE>
+__global__ __launch_bounds__(512, 2) void i8_few_sum(I8Args a, int stride) {
+  constexpr int DEPTH = 4, kAll = 8;
+  extern __shared__ char levels[];
+  __shared__ int sums[TACG_MAX_TOPK][kTileRows];
+  __shared__ float scales[TACG_MAX_TOPK];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int place = lane_place(a, blockIdx.x == 0 && blockIdx.y == 0);
+  const int t0 = blockIdx.y * a.k, n0 = blockIdx.x * kTileRows;
+  const uint64_t served = (__ballot(place >= 0) >> t0) & ((uint64_t(1) << a.k) - 1);
+  for (int i = tid; i < TACG_MAX_TOPK * kTileRows; i += 512) sums[i / kTileRows][i % kTileRows] = 0;
+  int slots = 0;
+  for (uint64_t m = served; m != 0; m &= m - 1, ++slots) {
+    const int j = __ffsll(static_cast<unsigned long long>(m)) - 1;
+    if (!a.slots && slots > 0) continue;  // one x for all
+    if (slots % kAll != wave) continue;
+    const float s = round_to_lds<DTYPE, 64>(a, blockIdx.y * a.x_token + j * a.x_slot, a.slots ? t0 + j : blockIdx.y, levels + slots * stride,
+                                            nullptr, lane, blockIdx.x == 0);
+    if (lane == 0) scales[slots] = s;
+  }
+  __syncthreads();
+  const int all = slots * a.col_tiles, begin = all * wave / kAll, end = all * (wave + 1) / kAll;
+  const int row = min(n0 + (lane & 15), a.row_tiles * kTileRows - 1);
+  const uint32_t at = static_cast<uint32_t>(row / kTileRows) * a.col_tiles * kTileBytes + (lane >> 4) * 256 + row % kTileRows * kPiece;
+  uint64_t left = served;
+  int slot = 0;
+  for (int c = begin; c < end;) {
+    while (c >= (slot + 1) * a.col_tiles) left &= left - 1, ++slot;
+    const int j = __ffsll(static_cast<unsigned long long>(left)) - 1;
+    const char* w = matrix_of(a, __builtin_amdgcn_readlane(place, t0 + j));
+    const char* token = levels + (a.slots ? slot : 0) * stride + (lane >> 4) * kPiece;
+    const int base = slot * a.col_tiles, stop = min(end, base + a.col_tiles);
+    int4v acc = {0, 0, 0, 0};
+    for (; c < stop; c += 2 * DEPTH) {
+      int4v v[2 * DEPTH];
+#pragma unroll
+      for (int d = 0; d < 2 * DEPTH; ++d) v[d] = load16(w + (at + static_cast<uint32_t>(min(c + d, stop - 1) - base) * kTileBytes));
+#pragma unroll
+      for (int d = 0; d < 2 * DEPTH; ++d)
+        if (c + d < stop) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[d], load16(token + (c + d - base) * kTileCols), acc, 0, 0, 0);
+    }
+    c = stop;
+    if ((lane & 15) == 0) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) atomicAdd(&sums[slot][(lane >> 4) * 4 + r], acc[r]);
+    }
+  }
+  barrier_after_lds_atomics();
+  const int n = n0 + tid;
+  if (tid >= kTileRows || n >= a.N) return;
+  float y = 0.0f;
+  int s = 0;
+  for (uint64_t m = served; m != 0; m &= m - 1, ++s) {
+    const int j = __ffsll(static_cast<unsigned long long>(m)) - 1, h = __builtin_amdgcn_readlane(place, t0 + j);
+    const float v = static_cast<float>(sums[s][tid]) * (scales[a.slots ? s : 0] * a.w_scale[static_cast<int64_t>(h) * a.N + n]);
+    y += (a.gate != nullptr ? a.gate[t0 + j] : 1.0f) * v;
+  }
+  store(a.out, static_cast<int64_t>(blockIdx.y) * a.N + n, y, a.out_dtype);
+}
+
 // Sums over the slots of a token, in order.  grid: (blocks of 1024 output columns, tokens).
 __global__ __launch_bounds__(256) void i8_combine(I8Args a) {
   const int n = (blockIdx.x * 256 + threadIdx.x) * 4, lane = threadIdx.x & 63;
@@ -754,6 +978,33 @@ TokenArgs token_args(const void* x, int64_t stride_token, int64_t stride_slot, i
 // Pairs of a tile: whether so few fall to a matrix, on average, that their time is that of the weights' loads.
 int tile_of(int64_t pairs, int32_t n_experts) { return pairs <= 24 * static_cast<int64_t>(n_experts) ? kFewTile : kManyTile; }
 
+// Few pairs, whose tokens' levels find room in LDS: one launch.  Rows of levels are 16 bytes further apart than they are long, so that
+// the same column of neighbours lies in different banks.
+struct Few {
+  bool is;
+  int stride;
+  uint32_t lds;
+};
+Few few_of(int64_t n_tokens, int32_t top_k, int32_t n_cols, int32_t mode, bool slots) {
+  Few f{};
+  const int64_t pairs = n_tokens * top_k;
+  f.stride = (n_cols + kTileCols - 1) / kTileCols * kTileCols + 16;
+  const int64_t rows = mode == TACG_Q4_SUM ? (slots ? top_k : 1) : std::min<int64_t>(n_tokens * (slots ? top_k : 1), 16);
+  f.is = pairs <= kFewPairs && rows * f.stride <= 49152;
+  f.lds = static_cast<uint32_t>(rows * f.stride);
+  return f;
+}
+
+template <int DTYPE>
+void start_few(const I8Args& a, const Few& f, hipStream_t stream) {
+  if (a.mode == TACG_Q4_SUM) {
+    i8_few_sum<DTYPE><<<dim3(a.row_tiles, static_cast<uint32_t>(a.n_tokens)), 512, f.lds, stream>>>(a, f.stride);
+    return;
+  }
+  const int width = a.mode == TACG_Q4_GLU ? a.N / 2 : a.N, rows = a.mode == TACG_Q4_GLU ? kTileRows : 2 * kTileRows;
+  i8_few<DTYPE><<<dim3((width + rows - 1) / rows, static_cast<uint32_t>(a.n_tokens * a.k)), 256, f.lds, stream>>>(a, rows, f.stride);
+}
+
 // The parts of a call's workspace.
 struct Space {
   int8_t* levels;
@@ -766,6 +1017,7 @@ struct Space {
 Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
                bool slots) {
   Space s{};
+  if (few_of(n_tokens, top_k, n_cols, mode, slots).is) return s;
   Carver ws{static_cast<char*>(base), 0};
   const int64_t pairs = n_tokens * top_k, rows = slots ? pairs : n_tokens;
   if (dtype != TACG_I8) {
@@ -828,6 +1080,7 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
   a.E = n_experts;
   a.H = n_held;
   a.N = n_rows;
+  a.K = n_cols;
   a.row_tiles = (n_rows + kTileRows - 1) / kTileRows;
   a.col_tiles = (n_cols + kTileCols - 1) / kTileCols;
   a.mode = mode;
@@ -841,6 +1094,18 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
   a.part = s.part;
   a.out = out;
   a.err = d_err;
+  const Few few_pairs = few_of(n_tokens, top_k, n_cols, mode, slots);
+  if (few_pairs.is) {
+    a.tokens = x;
+    a.x_scale = x_scale;
+    a.x_token = stride_token;
+    a.x_slot = stride_slot;
+    if (dtype == TACG_I8) start_few<TACG_I8>(a, few_pairs, stream);
+    else if (dtype == TACG_F32) start_few<TACG_F32>(a, few_pairs, stream);
+    else if (dtype == TACG_BF16) start_few<TACG_BF16>(a, few_pairs, stream);
+    else start_few<TACG_F16>(a, few_pairs, stream);
+    return hipGetLastError() == hipSuccess ? TACG_OK : TACG_E_DEVICE;
+  }
   // rows of a workgroup: fewer where the grid would leave processors idle
   const bool few = s.plan.tile == kFewTile;
   const int64_t busy = ids == nullptr ? (n_tokens + s.plan.tile - 1) / s.plan.tile * n_held

@@ -442,7 +442,8 @@ int tacg_i8_pack(const void* w, int32_t dtype, int32_t n_matrices, int32_t n_row
  * of the slots, and the result is rounded once: it depends on nothing but its token, its weights and its gates.  A token with a
  * value that is not finite gives NaN in its products, and sets TACG_ERR_VALUE; other data errors are those of tacg_expert_q4.  Tokens
  * and weights may be anything else that 32-bit products of the scales can hold.  workspace: tacg_expert_i8_workspace_bytes(...) bytes
- * (NULL where that is 0).  n_rows, n_cols <= TACG_MAX_WIDTH; n_held <= TACG_MAX_EXPERTS; T * k < 2^27.
+ * (NULL where that is 0).  n_rows, n_cols <= TACG_MAX_WIDTH; n_held <= TACG_MAX_EXPERTS; T * k < 2^27; the levels of all tokens span
+ * less than 2^36 bytes, and the results fewer than 2^39 tiles' elements (else TACG_E_UNSUPPORTED).
  */
 int tacg_expert_i8(const void* x, int32_t dtype, const float* x_scale_or_null, int64_t stride_token, int64_t stride_slot,
                    int64_t n_tokens, int32_t top_k, int32_t n_experts, const int16_t* ids_or_null,

@@ -464,12 +464,13 @@ __device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Uni
          [&](int, int pair) { return a.x_scale[a.slots ? pair : token_index(a, pair)]; });
 }
 
-// Many tokens: a wave has 64 weight rows and all tokens of the tile, JT blocks of 16.  Steps of 64 columns: weights go from memory to the
-// registers of the wave that needs them, three steps ahead; tokens through LDS, two steps ahead, and from there two blocks ahead.
+// Many tokens: a wave has 64 weight rows and all tokens of the tile, JT blocks of 16.  Weights go from memory to the registers of the wave that
+// needs them, three steps of 64 columns ahead.  Tokens go through LDS, whole lines of 128 bytes for two steps at a time, and from
+// there two blocks ahead.
 template <int JT>
 __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, const Unit& u, char* lds) {
-  constexpr int RF = 4, AHEAD = 2, kLoads = (JT + kWaves - 1) / kWaves;  // blocks of tokens that a wave brings in a step
-  constexpr int kStage = JT * kBlockBytes;
+  constexpr int RF = 4, AHEAD = 2, kLoads = JT / 2;  // loads of a wave for two steps: eight tokens each
+  constexpr int kHalf = JT * kBlockBytes + 16;       // LDS of a step; with 16 bytes more, the eight lanes of a token meet no bank twice
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool glu = a.mode == TACG_Q4_GLU;
   const int width = glu ? a.N / 2 : a.N;
@@ -477,10 +478,10 @@ __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, con
   const char* w = matrix_of(a, u.h);
   uint32_t at[RF];
   weight_rows<RF>(a, n0, glu, width, at);
-  const int8_t* token[kLoads];
+  uint32_t token[kLoads];  // in pieces of 16 bytes
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i)  // four neighbouring lanes share a token: 64 bytes of a line at a time
-    token[i] = token_of(a, pair_of(a, p, u, min((wave + i * kWaves) * 16 + (lane >> 2), u.count - 1))) + (lane & 3) * kPiece;
+  for (int i = 0; i < kLoads; ++i)
+    token[i] = static_cast<uint32_t>((token_of(a, pair_of(a, p, u, min((wave + i * kWaves) * 8 + (lane >> 3), u.count - 1))) - a.x) / kPiece);
   int4v acc[RF][JT];
 #pragma unroll
   for (int i = 0; i < RF; ++i)
@@ -492,33 +493,31 @@ __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, con
 #pragma unroll
     for (int i = 0; i < RF; ++i) v[i] = load16(w + (at[i] + from));
   };
-  auto load_tokens = [&](int c, int4v (&v)[kLoads]) {
+  int4v tk[kLoads];
+  auto load_tokens = [&](int c) {  // for steps c and c + 1; past the last column its own bytes again
+    const int from = min(c * kTileCols + (lane & 7) * kPiece, last * kTileCols + (lane & 3) * kPiece);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) v[i] = load16(token[i] + min(c, last) * kTileCols);
+    for (int i = 0; i < kLoads; ++i) tk[i] = load16(a.x + static_cast<uint64_t>(token[i]) * kPiece + from);
   };
-  auto keep_tokens = [&](int c, const int4v (&v)[kLoads]) {
+  auto keep_tokens = [&](int c) {
+    char* to = lds + ((c >> 1) & 1) * (2 * kHalf) + ((lane >> 2) & 1) * kHalf + (lane & 3) * kPieceBytes;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int j = wave + i * kWaves;
-      if (JT % kWaves == 0 || j < JT) 
-        *reinterpret_cast<int4v*>(lds + (c & 1) * kStage + j * kBlockBytes + (lane & 3) * kPieceBytes + (lane >> 2) * 16) = v[i];
+      const int row = (wave + i * kWaves) * 8 + (lane >> 3);
+      *reinterpret_cast<int4v*>(to + (row >> 4) * kBlockBytes + (row & 15) * 16) = tk[i];
     }
   };
-  int4v w0[RF], w1[RF], w2[RF], w3[RF], t0[kLoads], t1[kLoads];
-  load_tokens(0, t0);
+  int4v w0[RF], w1[RF], w2[RF], w3[RF];
+  load_tokens(0);
   load_weights(0, w0);
-  load_tokens(1, t1);
   load_weights(1, w1);
   load_weights(2, w2);
-  keep_tokens(0, t0);
-  auto step = [&](int c, int4v (&now)[RF], int4v (&far)[RF], int4v (&after)[kLoads], const int4v (&next)[kLoads]) {
-    __syncthreads();
-    load_tokens(c + 2, after);
-    load_weights(c + 3, far);
-    const char* from = lds + (c & 1) * kStage + (lane >> 4) * kPieceBytes + (lane & 15) * 16;
+  keep_tokens(0);
+  auto multiply = [&](int c, const int4v (&now)[RF]) {
+    const char* from = lds + ((c >> 1) & 1) * (2 * kHalf) + (c & 1) * kHalf + (lane >> 4) * kPieceBytes + (lane & 15) * 16;
     int4v t[AHEAD];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j) t[j] = load16(from + min(j, JT - 1) * kBlockBytes);
+    for (int j = 0; j < AHEAD; ++j) t[j] = load16(from + j * kBlockBytes);
 #pragma unroll
     for (int j = 0; j < JT; ++j) {
       __builtin_amdgcn_sched_barrier(0);
@@ -527,18 +526,21 @@ __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, con
       if (j + AHEAD < JT) t[j % AHEAD] = load16(from + (j + AHEAD) * kBlockBytes);
     }
     __builtin_amdgcn_sched_barrier(0);
-    keep_tokens(c + 1, next);
   };
-  int c = 0;
-  for (; c + 4 <= last + 1; c += 4) {
-    step(c, w0, w3, t0, t1);
-    step(c + 1, w1, w0, t1, t0);
-    step(c + 2, w2, w1, t0, t1);
-    step(c + 3, w3, w2, t1, t0);
+  // two steps: `first` holds the weights of the earlier one and takes those of step c + 4, `third` those of c + 3
+  auto pair_of_steps = [&](int c, int4v (&first)[RF], const int4v (&second)[RF], int4v (&third)[RF]) {
+    __syncthreads();
+    load_tokens(c + 2);
+    load_weights(c + 3, third);
+    if (c <= last) multiply(c, first);
+    load_weights(c + 4, first);
+    if (c + 1 <= last) multiply(c + 1, second);
+    keep_tokens(c + 2);
+  };
+  for (int c = 0; c <= last; c += 4) {
+    pair_of_steps(c, w0, w1, w3);
+    pair_of_steps(c + 2, w2, w3, w1);
   }
-  if (c <= last) step(c, w0, w3, t0, t1);
-  if (c + 1 <= last) step(c + 1, w1, w0, t1, t0);
-  if (c + 2 <= last) step(c + 2, w2, w1, t0, t1);
   finish<RF, JT>(a, p, u, n0, acc);
 }
 
@@ -672,7 +674,7 @@ __device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int bloc
 
 // grid: tiles of pairs x blocks of output columns, then `clear` workgroups.
 __global__ __launch_bounds__(256, 2) void i8_tiles(I8Args a, Plan p, int blocks, int rows, int clear) {
-  __shared__ alignas(16) char lds[2 * (kManyTile / 16) * kBlockBytes];
+  __shared__ alignas(16) char lds[4 * (kManyTile / 16 * kBlockBytes + 16)];
   Unit u;
   if (!unit_of<kManyTile>(a, p, blocks, rows, clear, u)) return;
   const int jt = (u.count + 15) / 16;
@@ -849,7 +851,7 @@ __global__ __launch_bounds__(256, 2) void i8_few(I8Args a, int rows, int stride)
 // steps of all served slots are shared evenly, and a slot's (exact) sums meet in LDS.
 template <int DTYPE>
 __global__ __launch_bounds__(512, 2) void i8_few_sum(I8Args a, int stride) {
-  constexpr int DEPTH = 4, kAll = 8;
+  constexpr int DEPTH = 8, kAll = 8;
   extern __shared__ char levels[];
   __shared__ int sums[TACG_MAX_TOPK][kTileRows];
   __shared__ float scales[TACG_MAX_TOPK];
@@ -858,41 +860,48 @@ __global__ __launch_bounds__(512, 2) void i8_few_sum(I8Args a, int stride) {
   const int t0 = blockIdx.y * a.k, n0 = blockIdx.x * kTileRows;
   const uint64_t served = (__ballot(place >= 0) >> t0) & ((uint64_t(1) << a.k) - 1);
   for (int i = tid; i < TACG_MAX_TOPK * kTileRows; i += 512) sums[i / kTileRows][i % kTileRows] = 0;
-  int slots = 0;
-  for (uint64_t m = served; m != 0; m &= m - 1, ++slots) {
-    const int j = __ffsll(static_cast<unsigned long long>(m)) - 1;
-    if (!a.slots && slots > 0) continue;  // one x for all
-    if (slots % kAll != wave) continue;
-    const float s = round_to_lds<DTYPE, 64>(a, blockIdx.y * a.x_token + j * a.x_slot, a.slots ? t0 + j : blockIdx.y, levels + slots * stride,
-                                            nullptr, lane, blockIdx.x == 0);
-    if (lane == 0) scales[slots] = s;
-  }
-  __syncthreads();
-  const int all = slots * a.col_tiles, begin = all * wave / kAll, end = all * (wave + 1) / kAll;
+  // the wave's steps, and the weights of the first of them, which come while the tokens are rounded
+  const int slots = __popcll(served), all = slots * a.col_tiles, begin = all * wave / kAll, end = all * (wave + 1) / kAll;
   const int row = min(n0 + (lane & 15), a.row_tiles * kTileRows - 1);
   const uint32_t at = static_cast<uint32_t>(row / kTileRows) * a.col_tiles * kTileBytes + (lane >> 4) * 256 + row % kTileRows * kPiece;
   uint64_t left = served;
-  int slot = 0;
+  int slot = 0, stop = 0;
+  const char* w = nullptr;
+  int4v v[DEPTH];
+  auto load = [&](int c) {
+    if (c >= stop) {  // the matrix of another slot
+      while (c >= (slot + 1) * a.col_tiles) left &= left - 1, ++slot;
+      w = matrix_of(a, __builtin_amdgcn_readlane(place, t0 + __ffsll(static_cast<unsigned long long>(left)) - 1));
+      stop = min(end, (slot + 1) * a.col_tiles);
+    }
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) v[d] = load16(w + (at + static_cast<uint32_t>(min(c + d, stop - 1) - slot * a.col_tiles) * kTileBytes));
+  };
+  if (begin < end) load(begin);
+  int s0 = 0;
+  for (uint64_t m = served; m != 0; m &= m - 1, ++s0) {
+    const int j = __ffsll(static_cast<unsigned long long>(m)) - 1;
+    if ((!a.slots && s0 > 0) || s0 % kAll != wave) continue;  // one x for all slots, or one each
+    const float s = round_to_lds<DTYPE, 64>(a, blockIdx.y * a.x_token + j * a.x_slot, a.slots ? t0 + j : blockIdx.y, levels + s0 * stride,
+                                            nullptr, lane, blockIdx.x == 0);
+    if (lane == 0) scales[s0] = s;
+  }
+  __syncthreads();
+  int4v acc = {0, 0, 0, 0};
   for (int c = begin; c < end;) {
-    while (c >= (slot + 1) * a.col_tiles) left &= left - 1, ++slot;
-    const int j = __ffsll(static_cast<unsigned long long>(left)) - 1;
-    const char* w = matrix_of(a, __builtin_amdgcn_readlane(place, t0 + j));
-    const char* token = levels + (a.slots ? slot : 0) * stride + (lane >> 4) * kPiece;
-    const int base = slot * a.col_tiles, stop = min(end, base + a.col_tiles);
-    int4v acc = {0, 0, 0, 0};
-    for (; c < stop; c += 2 * DEPTH) {
-      int4v v[2 * DEPTH];
+    const char* token = levels + (a.slots ? slot : 0) * stride + (lane >> 4) * kPiece - slot * a.col_tiles * kTileCols;
 #pragma unroll
-      for (int d = 0; d < 2 * DEPTH; ++d) v[d] = load16(w + (at + static_cast<uint32_t>(min(c + d, stop - 1) - base) * kTileBytes));
+    for (int d = 0; d < DEPTH; ++d)
+      if (c + d < stop) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[d], load16(token + (c + d) * kTileCols), acc, 0, 0, 0);
+    c = min(c + DEPTH, stop);
+    if (c == stop) {
+      if ((lane & 15) == 0) {
 #pragma unroll
-      for (int d = 0; d < 2 * DEPTH; ++d)
-        if (c + d < stop) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[d], load16(token + (c + d - base) * kTileCols), acc, 0, 0, 0);
+        for (int r = 0; r < 4; ++r) atomicAdd(&sums[slot][(lane >> 4) * 4 + r], acc[r]);
+      }
+      acc = int4v{0, 0, 0, 0};
     }
-    c = stop;
-    if ((lane & 15) == 0) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) atomicAdd(&sums[slot][(lane >> 4) * 4 + r], acc[r]);
-    }
+    if (c < end) load(c);
   }
   barrier_after_lds_atomics();
   const int n = n0 + tid;
@@ -1106,6 +1115,11 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
     else start_few<TACG_F16>(a, few_pairs, stream);
     return hipGetLastError() == hipSuccess ? TACG_OK : TACG_E_DEVICE;
   }
+  // tokens are found by 32-bit numbers of their 16-byte pieces
+  const int64_t row = static_cast<int64_t>(a.col_tiles) * kTileCols;
+  const double span = dtype == TACG_I8 ? static_cast<double>(n_tokens) * stride_token + static_cast<double>(top_k) * stride_slot + row
+                                       : static_cast<double>(n_tokens) * (slots ? top_k : 1) * row;
+  if (span >= 0x1p36) return TACG_E_UNSUPPORTED;
   // rows of a workgroup: fewer where the grid would leave processors idle
   const bool few = s.plan.tile == kFewTile;
   const int64_t busy = ids == nullptr ? (n_tokens + s.plan.tile - 1) / s.plan.tile * n_held

@@ -642,7 +642,6 @@ __device__ __forceinline__ void clear_block(const I8Args& a, int block, int bloc
 
 // The unit of a workgroup: a tile of pairs and a block of `rows` output columns.  Neighbouring units share tokens or weights: each
 // of the eight dies takes a run of them, as workgroups go to the dies in turn.
-template <int TILE>
 __device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int blocks, int rows, int clear, Unit& u) {
   // tiles that there are: those of pairs served here
   const int total = (a.ids == nullptr ? p.n_tiles : p.number(__builtin_amdgcn_readfirstlane(p.first[a.H]), a.H)) * blocks;
@@ -657,9 +656,9 @@ __device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int bloc
   const int tile = w / blocks;
   u.n0 = (w - tile * blocks) * rows;
   if (a.ids == nullptr) {
-    const int per = (static_cast<int>(a.n_tokens) + TILE - 1) / TILE;
+    const int per = (static_cast<int>(a.n_tokens) + p.tile - 1) / p.tile;
     u.h = tile / per;
-    u.first = (tile - u.h * per) * TILE;
+    u.first = (tile - u.h * per) * p.tile;
     u.count = static_cast<int>(a.n_tokens) - u.first;
   } else {
     const int2 t = p.tiles[tile];
@@ -668,7 +667,7 @@ __device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int bloc
     if (u.h < 0) return false;
     u.count = __builtin_amdgcn_readfirstlane(p.first[u.h + 1]) - u.first;
   }
-  u.count = min(u.count, TILE);
+  u.count = min(u.count, p.tile);
   return true;
 }
 
@@ -676,7 +675,7 @@ __device__ __forceinline__ bool unit_of(const I8Args& a, const Plan& p, int bloc
 __global__ __launch_bounds__(256, 2) void i8_tiles(I8Args a, Plan p, int blocks, int rows, int clear) {
   __shared__ alignas(16) char lds[4 * (kManyTile / 16 * kBlockBytes + 16)];
   Unit u;
-  if (!unit_of<kManyTile>(a, p, blocks, rows, clear, u)) return;
+  if (!unit_of(a, p, blocks, rows, clear, u)) return;
   const int jt = (u.count + 15) / 16;
   if (jt > 6) tile_product<8>(a, p, u, lds);
   else if (jt > 4) tile_product<6>(a, p, u, lds);
@@ -688,7 +687,7 @@ template <int RF, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void i8_stream(I8Args a, Plan p, int blocks, int rows, int clear) {
   __shared__ int4v lds[SPLIT ? (kWaves - 1) * RF * 2 * 64 : 1];
   Unit u;
-  if (!unit_of<kFewTile>(a, p, blocks, rows, clear, u)) return;
+  if (!unit_of(a, p, blocks, rows, clear, u)) return;
   if (u.count > 16) stream_product<RF, 2, SPLIT>(a, p, u, lds);
   else stream_product<RF, 1, SPLIT>(a, p, u, lds);
 }
@@ -984,8 +983,24 @@ TokenArgs token_args(const void* x, int64_t stride_token, int64_t stride_slot, i
   return t;
 }
 
-// Pairs of a tile: whether so few fall to a matrix, on average, that their time is that of the weights' loads.
-int tile_of(int64_t pairs, int32_t n_experts) { return pairs <= 24 * static_cast<int64_t>(n_experts) ? kFewTile : kManyTile; }
+// Pairs of a tile.  So few a matrix, on average, that their time is that of the weights' loads: 32.  Else as many as a wave has registers for, or
+// fewer where that leaves fewer processors idle.  A processor's time is that of its workgroups' tokens and, for the start and the end of
+// each, of 128 tokens more if it has one, 45 if one of them works while another waits (at 2048 columns; measured on grids of 64 to 4500
+// workgroups).  In us, 128 / 96 / 64 pairs: 3001 tokens through one gated matrix of 4096 x 2048: 43 / 38 / 46; 800 through 8 of 4096 x
+// 2048: 38 / 32 / 36; 1500, top-2, through 16 of 2048 x 2048: 46 / 40 / 33; 8000, top-6, through 64 gated of 2816 x 2048: 336 / 350 / 400.
+int tile_of(int64_t pairs, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols, bool shared) {
+  if (pairs <= 24 * static_cast<int64_t>(n_experts)) return kFewTile;
+  const int64_t blocks = (n_rows + 4 * kWaves * kTileRows - 1) / (4 * kWaves * kTileRows);
+  const double here = static_cast<double>(pairs) * n_held / n_experts;  // on average
+  int best = kManyTile;
+  double least = 0.0;
+  for (int tile = kManyTile; tile >= 64; tile -= 32) {
+    const double tiles = shared ? static_cast<double>((pairs / n_held + tile - 1) / tile * n_held) : here / tile + 0.5 * n_held;
+    const double each = std::ceil(tiles * blocks / 256), cost = each * (tile + (each > 1.0 ? 45.0 : 128.0) * 2048 / n_cols);
+    if (tile == kManyTile || cost < 0.95 * least) best = tile, least = cost;
+  }
+  return best;
+}
 
 // Few pairs, whose tokens' levels find room in LDS: one launch.  Rows of levels are 16 bytes further apart than they are long, so that
 // the same column of neighbours lies in different banks.
@@ -1024,7 +1039,7 @@ struct Space {
 };
 
 Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
-               bool slots) {
+               bool slots, bool shared) {
   Space s{};
   if (few_of(n_tokens, top_k, n_cols, mode, slots).is) return s;
   Carver ws{static_cast<char*>(base), 0};
@@ -1033,12 +1048,12 @@ Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_experts, i
     s.levels = ws.take<int8_t>(rows * ((n_cols + kTileCols - 1) / kTileCols * kTileCols));
     s.scales = ws.take<float>(rows);
   }
-  s.plan.tile = tile_of(pairs, n_experts);
+  s.plan.tile = tile_of(pairs, n_experts, n_held, n_rows, n_cols, shared);  // `shared` does not change the bytes
   s.plan.sparse = pairs <= n_held;
   s.plan.n_tiles = s.plan.sparse ? static_cast<int32_t>(pairs) : static_cast<int32_t>(pairs / s.plan.tile + n_held);
   s.plan.order = ws.take<int32_t>(pairs);
   s.plan.first = ws.take<int32_t>(n_held + 1);
-  s.plan.tiles = ws.take<int2>(s.plan.n_tiles);
+  s.plan.tiles = ws.take<int2>(pairs / kFewTile + n_held);  // whatever the tile is
   if (mode == TACG_Q4_SUM && top_k > 1) s.part = ws.take<float>(pairs * n_rows);
   s.bytes = ws.used;
   return s;
@@ -1073,7 +1088,7 @@ int launch_token_i8(const void* x, int32_t dtype, int64_t row_stride, int64_t n_
 
 size_t expert_i8_workspace(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols,
                            int32_t mode, int32_t dtype, bool slots) {
-  return space_of(nullptr, n_tokens, top_k, n_experts, n_held, n_rows, n_cols, mode, dtype, slots).bytes;
+  return space_of(nullptr, n_tokens, top_k, n_experts, n_held, n_rows, n_cols, mode, dtype, slots, false).bytes;
 }
 
 int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t stride_token, int64_t stride_slot, int64_t n_tokens,
@@ -1081,7 +1096,7 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
                      const int8_t* w, const float* w_scale, int32_t n_rows, int32_t n_cols, int32_t mode, const float* gate,
                      void* out, int32_t out_dtype, uint32_t* d_err, void* workspace, hipStream_t stream) {
   const bool slots = stride_slot != 0;
-  Space s = space_of(workspace, n_tokens, top_k, ids != nullptr ? n_experts : n_held, n_held, n_rows, n_cols, mode, dtype, slots);
+  Space s = space_of(workspace, n_tokens, top_k, ids != nullptr ? n_experts : n_held, n_held, n_rows, n_cols, mode, dtype, slots, ids == nullptr);
   I8Args a{};
   a.n_tokens = n_tokens;
   a.k = top_k;

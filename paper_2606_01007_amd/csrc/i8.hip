@@ -983,15 +983,19 @@ TokenArgs token_args(const void* x, int64_t stride_token, int64_t stride_slot, i
   return t;
 }
 
-// Pairs of a tile.  So few a matrix, on average, that their time is that of the weights' loads: 32.  Else as many as a wave has registers for, or
+// Pairs of a tile.  So few a matrix, on average, that their time is that of the weights' loads, or so few workgroups that
+// most processors would idle: 32, streamed (streamed / tiles in us: gated, 128 experts of 1536 x 2048, top-8: 52 / 54 at 16 tokens, 65 / 71 at 32, 81 / 79
+// at 64, 104 / 88 at 512; one matrix of 4096 x 4096: 12 / 20 at 16, 16 / 27 at 64; 200 tokens, top-4,
+// 15 of 60 of 2048 x 1408, summed: 21.7 / 24.4).  Else as many as a wave has registers for, or
 // fewer where that leaves fewer processors idle.  A processor's time is that of its workgroups' tokens and, for the start and the end of
 // each, of 128 tokens more if it has one, 45 if one of them works while another waits (at 2048 columns; measured on grids of 64 to 4500
 // workgroups).  In us, 128 / 96 / 64 pairs: 3001 tokens through one gated matrix of 4096 x 2048: 43 / 38 / 46; 800 through 8 of 4096 x
 // 2048: 38 / 32 / 36; 1500, top-2, through 16 of 2048 x 2048: 46 / 40 / 33; 8000, top-6, through 64 gated of 2816 x 2048: 336 / 350 / 400.
 int tile_of(int64_t pairs, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols, bool shared) {
-  if (pairs <= 24 * static_cast<int64_t>(n_experts)) return kFewTile;
   const int64_t blocks = (n_rows + 4 * kWaves * kTileRows - 1) / (4 * kWaves * kTileRows);
   const double here = static_cast<double>(pairs) * n_held / n_experts;  // on average
+  const double grid = (here / 64 + 0.5 * n_held) * blocks;
+  if (pairs <= 3 * static_cast<int64_t>(n_experts) || grid < 64 || (grid < 128 && here <= 14.0 * n_held)) return kFewTile;
   int best = kManyTile;
   double least = 0.0;
   for (int tile = kManyTile; tile >= 64; tile -= 32) {
@@ -1002,19 +1006,24 @@ int tile_of(int64_t pairs, int32_t n_experts, int32_t n_held, int32_t n_rows, in
   return best;
 }
 
-// Few pairs, whose tokens' levels find room in LDS: one launch.  Rows of levels are 16 bytes further apart than they are long, so that
+// Few pairs, whose tokens' levels find room in LDS: one launch, as long as the tokens of a matrix, which are rounded one after another, are few
+// too, and, summed, few tokens read the same weights.  One / two launches in us: gated, 6 of 64 experts of 2816 x 2048: 10.5 / 13.2 at one
+// token, 34 / 38 at 8; 2 of 8 of 4096 x 2048: 9.8 / 13.0, 16.5 / 21.7 at 8, 21.8 / 19.0 at 16; one of 4096 x 4096: 9.0 / 12.1, 11.3 / 12.1 at 4,
+// 13.7 / 12.3 at 6; summed, 8 of 256 of 4096 x 1024: 9.7 / 16.1, 49 / 50 at 8; 2 of 8 of 4096 x 2048: 17 / 21 at 4, 23 / 22 at 6.  Rows of levels are 16 bytes further apart than they are long, so that
 // the same column of neighbours lies in different banks.
 struct Few {
   bool is;
   int stride;
   uint32_t lds;
 };
-Few few_of(int64_t n_tokens, int32_t top_k, int32_t n_cols, int32_t mode, bool slots) {
+Few few_of(int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_cols, int32_t mode, bool slots) {
   Few f{};
   const int64_t pairs = n_tokens * top_k;
   f.stride = (n_cols + kTileCols - 1) / kTileCols * kTileCols + 16;
   const int64_t rows = mode == TACG_Q4_SUM ? (slots ? top_k : 1) : std::min<int64_t>(n_tokens * (slots ? top_k : 1), 16);
-  f.is = pairs <= kFewPairs && rows * f.stride <= 49152;
+  const bool alone = mode == TACG_Q4_SUM ? pairs <= kFewPairs && n_tokens <= std::max(4, n_experts / top_k)
+                                         : pairs <= 48 && pairs <= 4 * static_cast<int64_t>(n_experts);
+  f.is = alone && rows * f.stride <= 49152;
   f.lds = static_cast<uint32_t>(rows * f.stride);
   return f;
 }
@@ -1041,7 +1050,7 @@ struct Space {
 Space space_of(void* base, int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols, int32_t mode, int32_t dtype,
                bool slots, bool shared) {
   Space s{};
-  if (few_of(n_tokens, top_k, n_cols, mode, slots).is) return s;
+  if (few_of(n_tokens, top_k, n_experts, n_cols, mode, slots).is) return s;
   Carver ws{static_cast<char*>(base), 0};
   const int64_t pairs = n_tokens * top_k, rows = slots ? pairs : n_tokens;
   if (dtype != TACG_I8) {
@@ -1118,7 +1127,7 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
   a.part = s.part;
   a.out = out;
   a.err = d_err;
-  const Few few_pairs = few_of(n_tokens, top_k, n_cols, mode, slots);
+  const Few few_pairs = few_of(n_tokens, top_k, ids != nullptr ? n_experts : n_held, n_cols, mode, slots);
   if (few_pairs.is) {
     a.tokens = x;
     a.x_scale = x_scale;

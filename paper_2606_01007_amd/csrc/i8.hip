@@ -187,16 +187,19 @@ __global__ __launch_bounds__(256) void i8_pack_kernel(PackArgs a) {
     const bool in = n < a.N;
     const int64_t row = h * a.N + n;
     uint32_t m = 0;
+    float v[kChunk] = {};
     if (in)
-      for (int c = sub; c < a.K; c += 16) m = max(m, __float_as_uint(load<DTYPE>(a.w, row * a.K + c)) & 0x7fffffffu);
+      for (int c = sub * kChunk; c < a.K; c += 16 * kChunk) {
+        load_chunk<DTYPE>(a.w, row * a.K, c, a.K, v);
+        m = largest(v, m);
+      }
     for (int o = 8; o >= 1; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o, 64)));
     const bool bad = m >= 0x7f800000u;
     const Rounder level(bad ? 0.0f : __uint_as_float(m));
-    int8_t* out = a.q + tile * a.col_tiles * kTileBytes + r * kPiece + sub;
-    for (int p = 0; p < a.col_tiles * (kTileCols / kPiece); ++p) {
-      const int c = p * kPiece + sub;
-      out[static_cast<int64_t>(p) * kTileRows * kPiece] =
-          in && c < a.K && !bad ? static_cast<int8_t>(level(load<DTYPE>(a.w, row * a.K + c)) & 0xffu) : int8_t(0);
+    int8_t* out = a.q + tile * a.col_tiles * kTileBytes + r * kPiece;
+    for (int c = sub * kChunk; c < a.col_tiles * kTileCols; c += 16 * kChunk) {
+      if (in) load_chunk<DTYPE>(a.w, row * a.K, c, a.K, v);
+      *reinterpret_cast<uint2*>(out + static_cast<int64_t>(c / kPiece) * kTileRows * kPiece + c % kPiece) = levels_of(level, v, bad || !in);
     }
     if (in && sub == 0) {
       a.scale[row] = bad ? NAN : __uint_as_float(m) / 127.0f;

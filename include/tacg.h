@@ -440,7 +440,7 @@ int tacg_i8_pack(const void* w, int32_t dtype, int32_t n_matrices, int32_t n_row
  * The modes are those of tacg_expert_q4, with W_h[n] . x = (x_scale * w_scale[h][n]) * sum over c of levels; gate NULL is a gate of 1.
  * out has type out_dtype (TACG_F32, TACG_BF16, TACG_F16).  Sums over columns are exact, those over slots are held in 32 bits in the order
  * of the slots, and the result is rounded once: it depends on nothing but its token, its weights and its gates.  A token with a
- * value that is not finite gives NaN in its products, and sets TACG_ERR_VALUE; other data errors are those of tacg_expert_q4.  Tokens
+ * value that is not finite gives NaN in its products, and sets TACG_ERR_VALUE (without a product here it may go unnoticed); other data errors are those of tacg_expert_q4.  Tokens
  * and weights may be anything else that 32-bit products of the scales can hold.  workspace: tacg_expert_i8_workspace_bytes(...) bytes
  * (NULL where that is 0).  n_rows, n_cols <= TACG_MAX_WIDTH; n_held <= TACG_MAX_EXPERTS; T * k < 2^27; the levels of all tokens span
  * less than 2^36 bytes, and the results fewer than 2^39 tiles' elements (else TACG_E_UNSUPPORTED).

@@ -695,6 +695,14 @@ def _row_tiles(N: int) -> int:
     return -(-N // 16)
 
 
+def _together(*tensors):
+    """All on the current device, whose stream the call uses."""
+    device = torch.cuda.current_device() if _device is None else _device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"expected tensors of the current device {device}, got one of {t.device}")
+
+
 def token_i8(x: torch.Tensor, err: Optional[torch.Tensor] = None, stream=None):
     """Tokens [...][K] in 8 bits (tacg_token_i8): levels int8 [...][K rounded up to 64] and scale float32 [...], with
     x ~ scale * levels.  Rows are contiguous and equally spaced.  A row with a value that is not finite gets the scale NaN and sets
@@ -705,9 +713,12 @@ def token_i8(x: torch.Tensor, err: Optional[torch.Tensor] = None, stream=None):
     if x.dtype not in DTYPES or not x.is_cuda or x.dim() < 1:
         raise ValueError(f"x: expected a float device tensor [...][K], got {x.dtype} {tuple(x.shape)}")
     lead, K = x.shape[:-1], x.shape[-1]
-    rows = x.reshape(-1, K) if x.is_contiguous() else x
+    rows = x.reshape(lead.numel(), K) if x.is_contiguous() else x
     if rows.dim() != 2 or (rows.stride(1) != 1 and K > 1):
         raise ValueError(f"x: expected contiguous rows that are equally spaced, got strides {x.stride()}")
+    if K < 1:
+        raise ValueError("x: expected rows of one value or more")
+    _together(x, err)
     q = torch.empty(lead + (-(-K // 64) * 64,), dtype=torch.int8, device=x.device)
     scale = torch.empty(lead, dtype=torch.float32, device=x.device)
     if err is None:
@@ -730,6 +741,7 @@ def i8_pack(weight: torch.Tensor, err: Optional[torch.Tensor] = None, stream=Non
                          f"{tuple(weight.shape)}")
     H, N, K = weight.shape
     dev = weight.device
+    _together(weight, err)
     q = torch.empty((H, _row_tiles(N), -(-K // 64), 4, 16, 16), dtype=torch.int8, device=dev)
     scale = torch.empty((H, N), dtype=torch.float32, device=dev)
     if err is None:
@@ -750,7 +762,7 @@ def expert_i8(x, ids: Optional[torch.Tensor], q: torch.Tensor, scale: torch.Tens
     call.  Or the pair of token_i8, for tokens that several calls take.  q, scale: the experts of this GPU (i8_pack).  ids,
     n_experts, slot_of_expert, mode and what they leave out are those of expert_q4; ids None: shared experts, every token takes all
     of q, slot j the j-th.  gate float32 [T][k], for "sum" (None: 1).  dtype: of the result (default: that of x or out, bfloat16
-    for a pair).  A token that is not finite gives NaN and sets ERR_VALUE in `err` (int32 [1], 0 at first; the calls of a program
+    for a pair).  A token that is not finite gives NaN in its products here, and sets ERR_VALUE if it has any, in `err` (int32 [1], 0 at first; the calls of a program
     can share one); ids out of range and bad entries of slot_of_expert set ERR_ID_RANGE and ERR_TABLE: without one nothing reports
     them."""
     if stream is not None:
@@ -794,6 +806,7 @@ def expert_i8(x, ids: Optional[torch.Tensor], q: torch.Tensor, scale: torch.Tens
     result = ((T, k, N), (T, k, N // 2), (T, N))[code]
     if out is None:
         out = torch.empty(result, dtype=dtype, device=x.device)
+    _together(x, x_scale, ids, q, scale, slot_of_expert, gate, ws, err, out)
     slot_stride = stride[1] if len(shape) == 3 else 0
     C = _lib or lib()
     need = C.tacg_expert_i8_workspace_bytes(T, k, E, H, N, K, code, kind, 1 if slot_stride else 0)

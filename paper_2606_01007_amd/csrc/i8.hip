@@ -4,9 +4,23 @@
 //
 // with levels -127..127, half to even, of 127 x / max |x|.  The sum is exact in 32 bits: its magnitude is at most 65536 * 2^14 = 2^30.
 //
-// i8_tokens: levels and scales of tokens, a workgroup per row.
-// i8_pack_kernel: the same of weights, into the tiles that the products read: 16 rows x 64 columns, 16 bytes of each row after another.
-// i8_product: a lane per weight row, a workgroup per (token, slot), or summed per token.
+// Weights lie in tiles of 16 rows x 64 columns (tacg_i8_pack), so that a wave's load of 1 KB is one operand of v_mfma_i32_16x16x64: lane n + 16 q
+// supplies columns 16 q .. 16 q + 15 of row n, and of token n, and holds the sums of rows 4 q .. 4 q + 3 with token n.  Rows and tokens are
+// padded to 64 columns with zeros, so no product has a bound.
+//
+// i8_prepare: levels of the tokens, a wave a row, kept in registers between the search for the largest and the rounding (8192 x 4096 in
+//   bfloat16: 27 us, 3.8 TB/s), and in the same launch the pairs in the order of their matrices (Plan; 32768 pairs of 128 matrices:
+//   10 us, latency of one reading; bound by the longer of both).
+// i8_few, i8_few_sum: few pairs, one launch.  One token through six gated matrices of 2816 x 2048: 8.8 us, 3.9 TB/s; through eight of 4096 x
+//   1024, summed: 9.6 us; bound by latency: each wave has eight (sixteen) steps, behind the list of the pairs and the rounding.
+// i8_stream: few pairs a matrix.  64 tokens, top-8, through 128 gated matrices of 1536 x 2048: 54 us, 7.4 TB/s of weights, a part of them from
+//   the last-level cache; bound by memory.
+// i8_tiles: many.  4096 x 4096 x 8192: 123 us, 2.2e15 operations/s (torch's int8 product of 8192^3 reaches 2.1e15); 4096 tokens, top-8,
+//   through 128 gated matrices of 1536 x 2048: 148 us, 1.4e15.  The matrix cores are busy half of the time; the caches give a CU 24 KB for
+//   each 64 columns of a tile, 11 TB/s in all (their first level is active 0.8 of the time), and random levels draw so much power
+//   that the clock falls from 2.4 to 2.0 GHz (the same product of zeros: 119 us against 162, run after run).
+// i8_combine: sums over the slots of a token, in order; 8190 tokens of 4096 columns, one of eight GPUs: 40 us, bound by memory.
+// i8_pack_kernel: 64 matrices of 2048 x 2048 in bfloat16 in 266 us, 3 TB/s; each row is read twice.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -758,7 +772,8 @@ __device__ __forceinline__ int lane_place(const I8Args& a, bool report) {
 template <int DTYPE>
 __global__ __launch_bounds__(256, 2) void i8_few(I8Args a, int rows, int stride) {
   constexpr int RF = 2, DEPTH = 4;
-  extern __shared__ char levels[];
+  extern __shared__ int4v levels_lds[];
+  char* levels = reinterpret_cast<char*>(levels_lds);
   __shared__ int4v sums[(kWaves - 1) * RF * 64];
   __shared__ int list[kFewPairs];
   __shared__ float scales[kFewPairs];
@@ -854,7 +869,8 @@ __global__ __launch_bounds__(256, 2) void i8_few(I8Args a, int rows, int stride)
 template <int DTYPE>
 __global__ __launch_bounds__(512, 2) void i8_few_sum(I8Args a, int stride) {
   constexpr int DEPTH = 8, kAll = 8;
-  extern __shared__ char levels[];
+  extern __shared__ int4v levels_lds[];
+  char* levels = reinterpret_cast<char*>(levels_lds);
   __shared__ int sums[TACG_MAX_TOPK][kTileRows];
   __shared__ float scales[TACG_MAX_TOPK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;

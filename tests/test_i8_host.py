@@ -87,7 +87,7 @@ def test_products_refuse(L):
     for kw in (dict(x=None), dict(x=odd(1)), dict(x=odd(2), dtype=0), dict(dtype=4), dict(dtype=-1), dict(xs=FAKE), dict(st=-1),
                dict(ss=-1), dict(T=-1), dict(k=0), dict(k=9), dict(E=0), dict(H=-1), dict(w=None), dict(w=odd(8)), dict(s=None),
                dict(s=odd(2)), dict(N=0), dict(K=0), dict(mode=3), dict(mode=-1), dict(mode=1, N=17), dict(out=None), dict(out=odd(1)),
-               dict(out=odd(2), od=0), dict(od=3), dict(err=None), dict(ws=None), dict(wsb=64), dict(ws=odd(64)),
+               dict(out=odd(2), od=0), dict(od=3), dict(err=None), dict(T=400, ws=None), dict(T=400, wsb=64), dict(T=400, ws=odd(64)),
                dict(ids=None), dict(ids=None, k=8, slot=FAKE),                                  # shared: k experts, no table
                dict(dtype=3), dict(dtype=3, xs=FAKE, x=odd(8)), dict(dtype=3, xs=FAKE, st=72), dict(dtype=3, xs=FAKE, ss=8),
                dict(dtype=3, xs=odd(2))):
@@ -99,9 +99,11 @@ def test_products_refuse(L):
 
 def test_workspace(L):
     need = lambda *a: L.tacg_expert_i8_workspace_bytes(*a)  # noqa: E731
-    assert need(4, 2, 8, 8, 16, 64, 0, 1, 0) % 256 == 0
-    assert need(4, 2, 8, 8, 16, 64, 0, 1, 0) >= 4 * 64 + 16
-    assert need(4, 2, 8, 8, 16, 65, 2, 1, 1) >= 8 * 128 + 32
+    assert need(4, 2, 8, 8, 16, 64, 0, 1, 0) == 0                                  # few pairs: none
+    assert need(400, 2, 8, 8, 16, 64, 0, 1, 0) % 256 == 0
+    assert need(400, 2, 8, 8, 16, 64, 0, 1, 0) >= 400 * 64 + 4 * 400 + 4 * 800     # levels, scales, the order of the pairs
+    assert need(400, 2, 8, 8, 16, 65, 2, 1, 1) >= 800 * 128 + 4 * 800 + 4 * 800 * 17
+    assert need(400, 2, 8, 8, 16, 64, 0, 3, 0) < 400 * 64                          # levels are there
     for bad in ((-1, 2, 8, 8, 16, 64, 0, 1, 0), (4, 0, 8, 8, 16, 64, 0, 1, 0), (4, 2, -1, 8, 16, 64, 0, 1, 0), (4, 2, 8, -1, 16, 64, 0, 1, 0),
                 (4, 2, 8, 8, 0, 64, 0, 1, 0), (4, 2, 8, 8, 16, 0, 0, 1, 0)):
         assert need(*bad) == 0

@@ -344,7 +344,8 @@ size_t tacg_route_workspace_bytes(int64_t n_tokens, int32_t n_layers, int32_t n_
  * largest score that have an available expert are kept, ties go to the lower number, and the k experts are chosen among theirs as tacg_route
  * chooses among all: fewer than k, and -1 in the slots behind, where those groups have fewer.  Scores, norm, counts and losses
  * are over all available experts, as there.  What 32 bits cannot order is ordered in 64: sums of scores, and scores with a bias, are
- * compared as 64-bit numbers where they are nearer than 32-bit ones can tell.  The backward pass is tacg_route_backward.  n_groups = 1 is tacg_route, with its order in 32 bits.
+ * compared as 64-bit numbers where they are nearer than 32-bit ones can tell.  The backward pass is tacg_route_backward.  n_groups = 1 is
+ * tacg_route, with its order in 32 bits.
  * 1 <= top_groups <= n_groups <= TACG_MAX_GROUPS (else TACG_E_UNSUPPORTED for more groups, TACG_E_INVAL otherwise).
  */
 int tacg_route_grouped(const void* logits, int32_t dtype, int64_t stride_layer, int64_t stride_token, int64_t n_tokens,

@@ -567,7 +567,8 @@ def route(logits: torch.Tensor, top_k: int, fam_off=None, score: str = "softmax"
         err = _err_tensor(logits.device)
     st = C.tacg_route_grouped(
         ptr, dtype, s_layer, s_token, N, L_, top_k, E, off, F, code,
-        _arg(bias, "bias", torch.float32, (L_, E)), 1 if renorm else 0, float(scale), groups, top_groups, group_best,
+        _arg(bias, "bias", torch.float32, (L_, E)), 1 if renorm else 0, float(scale), int(groups), int(top_groups),
+        int(group_best),
         _arg(out["trace"], "trace", torch.int16, (L_, N, top_k)), _arg(out["gate"], "gate", torch.float32, (L_, N, top_k)),
         _arg(out.get("norm"), "norm", torch.float32, (L_, N)), _arg(D, "D", torch.int32, (F, L_, E)),
         _arg(tokens, "tokens", torch.int32, (F, L_)), _arg(b, "balance", torch.float32, (F, L_)),

@@ -4,9 +4,10 @@
 // neighbouring 16-byte chunks go to LDS, a lane adds up a group's from there, and ranks it among the others.  Without a bias the values
 // are the logits, and only the best two of a group become scores.  All of it in 32 bits.
 // Rows whose order 32 bits may hold wrongly are left out, and taken again at the end, a wave a row, in 64 bits: where two groups' sums lie
-// nearer than near_by(), or, with a bias, two neighbours of the ordered list, the first that is not chosen among them; and rows with
-// more large values than the list holds.  Kept apart from the loop, so that neither its registers nor its time suffer (in the loop: 58 layers of
-// 8155 rows of 256 in 32 bits, biased sigmoid scores, top-8 in four of eight groups, 261 us against 232 at that time).
+// nearer than near_by(), or, with a bias, two neighbours of the ordered list, the first that is not chosen among them, unless their logits
+// and biases are equal; and rows with more large values than the list holds.  Kept apart from the loop, so that neither its registers nor its
+// time suffer (in the loop: 58 layers of 8155 rows of 256 in 32 bits, biased sigmoid scores, top-8 in four of eight groups, 261 us against
+// 232 at that time).
 // Those rows now: 186 us, 2.8 TB/s read, where all in 64 bits took 717; with sums and 4077 rows 136 us.  Bound by instruction issue (1235
 // vector instructions per eight rows, a fifth of them for the sigmoids, half of whose time is exp and reciprocal) and by waits for LDS: three
 // waves a SIMD, by registers (168) and LDS (50 KB).  With sums of biased scores ten registers spill, which costs less than the third
@@ -203,6 +204,7 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
       double list[kList];
       float2 chosen[KS * kRowLanes];
       float ranked[KL + 2];
+      int ranked_id[KL + 2];
     } after;
   };
   __shared__ Row rows[kRowsPerPass];
@@ -430,6 +432,7 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
     }
     int32_t* ids = reinterpret_cast<int32_t*>(mine);  // before the entries
     float* order = rows[tid >> 3].after.ranked;
+    int* order_id = rows[tid >> 3].after.ranked_id;
 #pragma unroll
     for (int q = 0; q < KS; ++q) slots[sub + q * kRowLanes] = make_float2(__int_as_float(-1), kNone);
     if constexpr (BIAS)
@@ -481,7 +484,7 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
       for (int q = 0; q < N; ++q) {
         if (sub + q * kRowLanes >= n) continue;
         if (larger[q] < k) slots[larger[q]] = make_float2(__int_as_float(e[q]), y[q]);
-        if (BIAS && larger[q] <= k) order[larger[q]] = v[q];
+        if (BIAS && larger[q] <= k) order[larger[q]] = v[q], order_id[larger[q]] = e[q];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
@@ -494,13 +497,19 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
     }
     int id[KS];   // of slots sub, sub + 8: expert and its logit
     float w[KS];
+    bool doubt = false;
+    auto close = [&](int j) { return order[j + 1] > kNone && order[j] - order[j + 1] <= near_by(order[j], most_bias, a.softmax); };
 #pragma unroll
     for (int q = 0; q < KS; ++q) {
       const int j = sub + q * kRowLanes;
       const float2 v = slots[j];
       id[q] = __float_as_int(v.x);
       w[q] = v.y;
-      if (BIAS && j < k) hard |= order[j + 1] > kNone && order[j] - order[j + 1] <= near_by(order[j], most_bias, a.softmax);
+      if (BIAS && j < k) doubt |= close(j);
+    }
+    if (BIAS && __any(doubt)) {  // equal logits with equal biases are equal, and in their order
+      for (int j = sub; j < k; j += kRowLanes)
+        if (close(j)) hard |= logit[order_id[j]] != logit[order_id[j + 1]] || bias_of[order_id[j]] != bias_of[order_id[j + 1]];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (__any(hard)) {

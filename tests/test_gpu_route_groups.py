@@ -254,3 +254,15 @@ def test_other_stream():
     got = tacg.route(x, 4, groups=8, top_groups=2, stream=side)
     side.synchronize()
     assert torch.equal(got["trace"], want["trace"]) and torch.equal(got["gate"], want["gate"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_equal_neighbours_with_equal_and_other_biases(dtype, score):
+    """Lists whose neighbours have equal logits: with equal biases they are in order as they are, with others 64 bits tell."""
+    g = torch.Generator().manual_seed(12)
+    x = (torch.randn((2, 300, 128), generator=g) * 2).mul(8).round().div(8).to(dtype)     # many equal pairs, few a row
+    for bias in (torch.zeros((2, 128)), torch.full((2, 128), -0.25), 2.0 ** -23 * torch.randint(-2, 3, (2, 128), generator=g).float(),
+                 torch.where(torch.rand((2, 128), generator=g) < 0.5, 0.0, 2.0 ** -24)):
+        for best in (1, 2):
+            _check(x, 8, score, bias, True, 1.0, 8, 4, best)

@@ -69,12 +69,6 @@ __device__ __forceinline__ int place_of(const I8Args& a, int64_t pair, int j) {
   return h < 0 ? -1 : h < a.H ? h : kBadTable;
 }
 
-template <int DTYPE>
-__device__ __forceinline__ float load(const void* p, int64_t i) {
-  if constexpr (DTYPE == TACG_F32) return static_cast<const float*>(p)[i];
-  else if constexpr (DTYPE == TACG_BF16) return static_cast<float>(static_cast<const __bf16*>(p)[i]);
-  else return static_cast<float>(static_cast<const _Float16*>(p)[i]);
-}
 __device__ __forceinline__ void store(void* p, int64_t i, float v, int dtype) {
   if (dtype == TACG_F32) static_cast<float*>(p)[i] = v;
   else if (dtype == TACG_BF16) static_cast<__bf16*>(p)[i] = static_cast<__bf16>(v);
@@ -353,8 +347,9 @@ __global__ __launch_bounds__(THREADS) void i8_prepare(TokenArgs t, I8Args a, Pla
 constexpr int kManyTile = 128, kFewTile = 32;  // pairs of a tile
 
 constexpr int kWaves = 4;
-// A block of 16 tokens in LDS: 16 bytes of each after another, for each quarter of the 64 columns; quarters are 18 * 16 bytes apart, so that
-// eight lanes that write all quarters of two tokens meet no bank twice.
+// A block of 16 tokens in LDS: 16 bytes of each after another, for each quarter of the 64 columns.  Quarters are 18 * 16 bytes apart and the
+// steps 16 more, as lanes that write different quarters of a token would meet the same banks: conflicts of a product of 4096 x 4096 x 8192
+// 3.3e4 cycles a CU of 2.5e5 (20 * 16 and 32: 4.9e4), which is not what bounds it.
 constexpr int kPieceBytes = 18 * 16, kBlockBytes = 4 * kPieceBytes;
 
 // What a lane does of its part of a tile's results: 4 consecutive rows of a token.
@@ -488,7 +483,7 @@ __device__ __forceinline__ void finish(const I8Args& a, const Plan& p, const Uni
 template <int JT>
 __device__ __forceinline__ void tile_product(const I8Args& a, const Plan& p, const Unit& u, char* lds) {
   constexpr int RF = 4, AHEAD = 2, kLoads = JT / 2;  // loads of a wave for two steps: eight tokens each
-  constexpr int kHalf = JT * kBlockBytes + 16;       // LDS of a step; with 16 bytes more, the eight lanes of a token meet no bank twice
+  constexpr int kHalf = JT * kBlockBytes + 16;       // LDS of a step
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool glu = a.mode == TACG_Q4_GLU;
   const int width = glu ? a.N / 2 : a.N;

@@ -203,8 +203,8 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
     struct {
       double list[kList];
       float2 chosen[KS * kRowLanes];
-      float ranked[KL + 2];
-      int ranked_id[KL + 2];
+      float ranked[KL + 1];
+      int next;  // the first that is not chosen
     } after;
   };
   __shared__ Row rows[kRowsPerPass];
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
     }
     int32_t* ids = reinterpret_cast<int32_t*>(mine);  // before the entries
     float* order = rows[tid >> 3].after.ranked;
-    int* order_id = rows[tid >> 3].after.ranked_id;
+    int& next = rows[tid >> 3].after.next;
 #pragma unroll
     for (int q = 0; q < KS; ++q) slots[sub + q * kRowLanes] = make_float2(__int_as_float(-1), kNone);
     if constexpr (BIAS)
@@ -484,7 +484,8 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
       for (int q = 0; q < N; ++q) {
         if (sub + q * kRowLanes >= n) continue;
         if (larger[q] < k) slots[larger[q]] = make_float2(__int_as_float(e[q]), y[q]);
-        if (BIAS && larger[q] <= k) order[larger[q]] = v[q], order_id[larger[q]] = e[q];
+        if (BIAS && larger[q] <= k) order[larger[q]] = v[q];
+        if (BIAS && larger[q] == k) next = e[q];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
@@ -508,8 +509,11 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
       if (BIAS && j < k) doubt |= close(j);
     }
     if (BIAS && __any(doubt)) {  // equal logits with equal biases are equal, and in their order
-      for (int j = sub; j < k; j += kRowLanes)
-        if (close(j)) hard |= logit[order_id[j]] != logit[order_id[j + 1]] || bias_of[order_id[j]] != bias_of[order_id[j + 1]];
+      for (int j = sub; j < k; j += kRowLanes) {
+        if (!close(j)) continue;
+        const int e = __float_as_int(slots[j].x), f = j + 1 < k ? __float_as_int(slots[j + 1].x) : next;
+        hard |= logit[e] != logit[f] || bias_of[e] != bias_of[f];
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (__any(hard)) {

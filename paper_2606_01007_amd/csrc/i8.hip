@@ -765,8 +765,9 @@ __device__ __forceinline__ int lane_place(const I8Args& a, bool report) {
   return h;
 }
 
-// Each and gated products: grid (blocks of 32 weight rows, pairs).  The workgroup of the first pair of a matrix takes all its pairs; its four
-// waves have a quarter of the columns each.  lds: rows of levels, `stride` bytes apart.
+// Each and gated products: grid (blocks of 32 weight rows, pairs).  The workgroup of the first pair of a matrix takes all its pairs, 16 at a
+// time; its four waves have a quarter of the columns each.  lds: rows of levels, `stride` bytes apart, as many as 16 pairs of a matrix can
+// have: one for each of up to 16 pairs, or, with one x for all slots, for each of up to 16 tokens (few_of).
 template <int DTYPE>
 __global__ __launch_bounds__(256, 2) void i8_few(I8Args a, int rows, int stride) {
   constexpr int RF = 2, DEPTH = 4;
@@ -807,14 +808,21 @@ __global__ __launch_bounds__(256, 2) void i8_few(I8Args a, int rows, int stride)
   // 16 tokens at a time
   for (int first = 0; first < u.count; first += 16) {
     const int n = min(u.count - first, 16);
-    for (int r = 0; r < n; ++r) {
-      const int pair = list[first + r], t = token_index(a, pair);
-      const float s = round_to_lds<DTYPE, 256>(a, t * a.x_token + (pair - t * a.k) * a.x_slot, a.slots ? pair : t, levels + r * stride, most,
-                                               tid, blockIdx.x == 0);
+    // a row of levels for each slot's x, or for each token: its pairs (an expert that it has twice, two experts with one matrix) are neighbours
+    uint32_t starts = 0;  // bit r: pair r is the first of a row
+    float s = 0.0f;
+    for (int r = 0, before = -1; r < n; ++r) {
+      const int pair = __builtin_amdgcn_readfirstlane(list[first + r]), t = token_index(a, pair);
+      if (a.slots || t != before) {
+        s = round_to_lds<DTYPE, 256>(a, t * a.x_token + (pair - t * a.k) * a.x_slot, a.slots ? pair : t, levels + __popc(starts) * stride, most,
+                                     tid, blockIdx.x == 0);
+        starts |= 1u << r;
+        before = t;
+      }
       if (tid == 0) scales[r] = s;
     }
     __syncthreads();
-    const char* token = levels + min(lane & 15, n - 1) * stride + (lane >> 4) * kPiece;
+    const char* token = levels + (__popc(starts & ((2u << min(lane & 15, n - 1)) - 1)) - 1) * stride + (lane >> 4) * kPiece;
     int4v acc[RF][1] = {};
     auto multiply = [&](int c, int d) {
       const int4v t = load16(token + c * kTileCols);

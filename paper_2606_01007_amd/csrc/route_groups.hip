@@ -4,8 +4,8 @@
 // neighbouring 16-byte chunks go to LDS, a lane adds up a group's from there, and ranks it among the others.  Without a bias the values
 // are the logits, and only the best two of a group become scores.  All of it in 32 bits.
 // Rows whose order 32 bits may hold wrongly are left out, and taken again at the end, a wave a row, in 64 bits: where two groups' sums lie
-// nearer than near_by(), or, with a bias, two neighbours of the ordered list, the first that is not chosen among them, unless their logits
-// and biases are equal; and rows with more large values than the list holds.  Kept apart from the loop, so that neither its registers nor its
+// nearer than near_by(), or, with a bias, two neighbours of those that are chosen, or the last of them and any that is not, unless their
+// logits and biases are equal; and rows with more large values than the list holds.  Kept apart from the loop, so that neither its registers nor its
 // time suffer (in the loop: 58 layers of 8155 rows of 256 in 32 bits, biased sigmoid scores, top-8 in four of eight groups, 261 us against
 // 232 at that time).
 // Those rows now: 186 us, 2.8 TB/s read, where all in 64 bits took 717; with sums and 4077 rows 136 us.  Bound by instruction issue (1235
@@ -204,7 +204,6 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
       double list[kList];
       float2 chosen[KS * kRowLanes];
       float ranked[KL + 1];
-      int next;  // the first that is not chosen
     } after;
   };
   __shared__ Row rows[kRowsPerPass];
@@ -432,7 +431,6 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
     }
     int32_t* ids = reinterpret_cast<int32_t*>(mine);  // before the entries
     float* order = rows[tid >> 3].after.ranked;
-    int& next = rows[tid >> 3].after.next;
 #pragma unroll
     for (int q = 0; q < KS; ++q) slots[sub + q * kRowLanes] = make_float2(__int_as_float(-1), kNone);
     if constexpr (BIAS)
@@ -485,7 +483,6 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
         if (sub + q * kRowLanes >= n) continue;
         if (larger[q] < k) slots[larger[q]] = make_float2(__int_as_float(e[q]), y[q]);
         if (BIAS && larger[q] <= k) order[larger[q]] = v[q];
-        if (BIAS && larger[q] == k) next = e[q];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
@@ -509,10 +506,17 @@ __global__ __launch_bounds__(kRouteThreads, 3) void route_grouped(RouteArgs a) {
       if (BIAS && j < k) doubt |= close(j);
     }
     if (BIAS && __any(doubt)) {  // equal logits with equal biases are equal, and in their order
-      for (int j = sub; j < k; j += kRowLanes) {
-        if (!close(j)) continue;
-        const int e = __float_as_int(slots[j].x), f = j + 1 < k ? __float_as_int(slots[j + 1].x) : next;
-        hard |= logit[e] != logit[f] || bias_of[e] != bias_of[f];
+      auto differ = [&](int e, int f) { return logit[e] != logit[f] || bias_of[e] != bias_of[f]; };
+      for (int j = sub; j + 1 < k; j += kRowLanes)
+        if (close(j)) hard |= differ(__float_as_int(slots[j].x), __float_as_int(slots[j + 1].x));
+      if (close(k - 1)) {  // one that is as near to the last chosen may stand behind equal ones: all that are not chosen
+        const int e = __float_as_int(slots[k - 1].x);
+        const float last = order[k - 1], near = near_by(last, most_bias, a.softmax);
+        for (int i = sub; i < n; i += kRowLanes) {
+          const double u = mine[i];
+          const float v = static_cast<float>(u);
+          if (v <= last && last - v <= near) hard |= differ(e, expert_of(u));
+        }
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

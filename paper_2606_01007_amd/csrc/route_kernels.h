@@ -257,6 +257,10 @@ __device__ __forceinline__ double entry_of(float v, int e) {
   const uint64_t bits = __builtin_bit_cast(uint64_t, static_cast<double>(v + 0.0f));  // -0 and +0 are equal
   return __builtin_bit_cast(double, bits | static_cast<uint32_t>(v < 0.0f ? e : 255 - e));
 }
+__device__ __forceinline__ int expert_of(double entry) {  // the id of a list entry, whose value is static_cast<float>(entry)
+  const int low = static_cast<int>(__builtin_bit_cast(uint64_t, entry) & 255u);
+  return entry < 0.0 ? low : 255 - low;
+}
 struct Run {
   int family;
   int64_t first, last;  // tokens

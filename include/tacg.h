@@ -442,8 +442,10 @@ int tacg_i8_pack(const void* w, int32_t dtype, int32_t n_matrices, int32_t n_row
  * of the slots, and the result is rounded once: it depends on nothing but its token, its weights and its gates.  A token with a
  * value that is not finite gives NaN in its products, and sets TACG_ERR_VALUE (without a product here it may go unnoticed); other data errors are those of tacg_expert_q4.  Tokens
  * and weights may be anything else that 32-bit products of the scales can hold.  workspace: tacg_expert_i8_workspace_bytes(...) bytes
- * (NULL where that is 0).  n_rows, n_cols <= TACG_MAX_WIDTH; n_held <= TACG_MAX_EXPERTS; T * k < 2^27; the levels of all tokens span
- * less than 2^36 bytes, and the results fewer than 2^39 tiles' elements (else TACG_E_UNSUPPORTED).
+ * (NULL where that is 0).  A token may have an expert in several slots, and several experts may have one matrix: each slot is a product.
+ * n_rows, n_cols <= TACG_MAX_WIDTH; n_held <= TACG_MAX_EXPERTS; T * k < 2^27; the levels of all tokens span less than 2^36 bytes (else
+ * TACG_E_UNSUPPORTED).  No call with (T * k / 64 + n_held) * ceil(n_rows / 256) < 2^24 - 512 is refused for the size of its results;
+ * beyond that TACG_E_UNSUPPORTED may come back, before any launch.
  */
 int tacg_expert_i8(const void* x, int32_t dtype, const float* x_scale_or_null, int64_t stride_token, int64_t stride_slot,
                    int64_t n_tokens, int32_t top_k, int32_t n_experts, const int16_t* ids_or_null,

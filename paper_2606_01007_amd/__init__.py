@@ -762,7 +762,8 @@ def expert_i8(x, ids: Optional[torch.Tensor], q: torch.Tensor, scale: torch.Tens
     x [T][K], or [T][k][K] where every slot has its own, rows contiguous, in bfloat16, float16 or float32: rounded to 8 bits in the
     call.  Or the pair of token_i8, for tokens that several calls take.  q, scale: the experts of this GPU (i8_pack).  ids,
     n_experts, slot_of_expert, mode and what they leave out are those of expert_q4; ids None: shared experts, every token takes all
-    of q, slot j the j-th.  gate float32 [T][k], for "sum" (None: 1).  dtype: of the result (default: that of x or out, bfloat16
+    of q, slot j the j-th.  K is that of the weights: packed weights tell it up to the next multiple of 64 only, and within that, columns
+    that x lacks count as 0.  gate float32 [T][k], for "sum" (None: 1).  dtype: of the result (default: that of x or out, bfloat16
     for a pair).  A token that is not finite gives NaN in its products here, and sets ERR_VALUE if it has any, in `err` (int32 [1], 0 at first; the calls of a program
     can share one); ids out of range and bad entries of slot_of_expert set ERR_ID_RANGE and ERR_TABLE: without one nothing reports
     them."""

@@ -1187,7 +1187,7 @@ int launch_expert_i8(const void* x, int32_t dtype, const float* x_scale, int64_t
                    static_cast<double>(n_tokens) * top_k >= 1.5 * s.plan.tile * (ids != nullptr ? n_experts : n_held);
   const int clear = ids != nullptr && s.part == nullptr ? static_cast<int>(std::min<int64_t>((n_tokens * top_k + 255) / 256, 512)) : 0;
   const int64_t grid = static_cast<int64_t>(s.plan.n_tiles) * blocks + clear;
-  if (grid >= (int64_t(1) << 32) / 256) return TACG_E_UNSUPPORTED;  // threads that a launch holds; results of more than 288 GB
+  if (grid >= (int64_t(1) << 32) / 256) return TACG_E_UNSUPPORTED;  // threads that a launch holds; so large a grid has tiles of 64 pairs or more
   const int n_plan = ids != nullptr ? std::max(n_held, 1) : 0;
   if (dtype == TACG_I8) {
     a.x = static_cast<const int8_t*>(x);

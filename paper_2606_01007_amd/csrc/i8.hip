@@ -9,17 +9,19 @@
 // padded to 64 columns with zeros, so no product has a bound.
 //
 // i8_prepare: levels of the tokens, a wave a row, kept in registers between the search for the largest and the rounding (8192 x 4096 in
-//   bfloat16: 27 us, 3.8 TB/s), and in the same launch the pairs in the order of their matrices (Plan; 32768 pairs of 128 matrices:
-//   10 us, latency of one reading; bound by the longer of both).
+//   bfloat16: 23 us, 4.4 TB/s, a part from the last-level cache; rows of more than 4096 columns are read twice: 8192 x 7168 53 us, 3.3 TB/s),
+//   and in the same launch the pairs in the order of their matrices (Plan; 32768 pairs of 128 matrices: 10 us, latency of one reading;
+//   bound by the longer of both).
 // i8_few, i8_few_sum: few pairs, one launch.  One token through six gated matrices of 2816 x 2048: 8.8 us, 3.9 TB/s; through eight of 4096 x
 //   1024, summed: 8.3 us; bound by latency: each wave has eight (sixteen) steps, behind the list of the pairs and the rounding.
-// i8_stream: few pairs a matrix.  64 tokens, top-8, through 128 gated matrices of 1536 x 2048: 54 us, 7.4 TB/s of weights, a part of them from
-//   the last-level cache; bound by memory.
-// i8_tiles: many.  4096 x 4096 x 8192: 123 us, 2.2e15 operations/s (torch's int8 product of 8192^3 reaches 2.1e15); 4096 tokens, top-8,
-//   through 128 gated matrices of 1536 x 2048: 148 us, 1.4e15.  The matrix cores are busy half of the time; the caches give a CU 24 KB for
-//   each 64 columns of a tile, 11 TB/s in all (their first level is active 0.8 of the time), and random levels draw so much power
-//   that the clock falls from 2.4 to 2.0 GHz (the same product of zeros: 119 us against 162, run after run).
-// i8_combine: sums over the slots of a token, in order; 8190 tokens of 4096 columns, one of eight GPUs: 40 us, bound by memory.
+// i8_stream: few pairs a matrix.  16 tokens, top-8, through 128 gated matrices of 1536 x 2048, of which they meet about 82: 46 us, 5.6 TB/s of
+//   weights; bound by memory.
+// i8_tiles: many.  64 tokens through those matrices: 74 us, 5.4 TB/s; bound by memory.  4096 x 4096 x 8192: 124 us, 2.2e15 operations/s
+//   (torch's int8 product of 8192^3 reaches 2.1e15); 4096 tokens, top-8, through the 128 matrices: 150 us, 1.4e15.  The matrix cores are
+//   busy half of the time; the caches give a CU 24 KB for each 64 columns of a tile, 11 TB/s in all (their first level is active 0.8 of the
+//   time), and random levels draw so much power that the clock falls from 2.4 to 2.0 GHz (the same product of zeros: 119 us against 162, run
+//   after run).
+// i8_combine: sums over the slots of a token, in order; 8190 tokens of 4096 columns, one of eight GPUs: 55 us, 3.7 TB/s; bound by memory.
 // i8_pack_kernel: 64 matrices of 2048 x 2048 in bfloat16 in 266 us, 3 TB/s; each row is read twice.
 #include <algorithm>
 #include <cmath>
@@ -1010,13 +1012,13 @@ TokenArgs token_args(const void* x, int64_t stride_token, int64_t stride_slot, i
 }
 
 // Pairs of a tile.  So few a matrix, on average, that their time is that of the weights' loads, or so few workgroups that
-// most processors would idle: 32, streamed (streamed / tiles in us: gated, 128 experts of 1536 x 2048, top-8: 52 / 54 at 16 tokens, 65 / 71 at 32, 81 / 79
-// at 64, 104 / 88 at 512; one matrix of 4096 x 4096: 12 / 20 at 16, 16 / 27 at 64; 200 tokens, top-4,
-// 15 of 60 of 2048 x 1408, summed: 21.7 / 24.4).  Else as many as a wave has registers for, or
+// most processors would idle: 32, streamed (calls in a row, streamed / tiles in us: gated, 128 experts of 1536 x 2048, top-8: 51 / 55 at 16
+// tokens, 72 / 71 at 32, 81 / 78 at 64, 104 / 87 at 512; one matrix of 4096 x 4096: 13 / 20 at 16, 16 / 27 at 64; 200 tokens, top-4,
+// 15 of 60 of 2048 x 1408, summed: 21.0 / 22.1).  Else as many as a wave has registers for, or
 // fewer where that leaves fewer processors idle.  A processor's time is that of its workgroups' tokens and, for the start and the end of
 // each, of 128 tokens more if it has one, 45 if one of them works while another waits (at 2048 columns; measured on grids of 64 to 4500
-// workgroups).  In us, 128 / 96 / 64 pairs: 3001 tokens through one gated matrix of 4096 x 2048: 43 / 38 / 46; 800 through 8 of 4096 x
-// 2048: 38 / 32 / 36; 1500, top-2, through 16 of 2048 x 2048: 46 / 40 / 33; 8000, top-6, through 64 gated of 2816 x 2048: 336 / 350 / 400.
+// workgroups).  In us, 128 / 96 / 64 pairs: 3001 tokens through one gated matrix of 4096 x 2048: 42 / 38 / 40; 800 through 8 of 4096 x
+// 2048: 35 / 30 / 36; 1500, top-2, through 16 of 2048 x 2048: 44 / 39 / 33; 8000, top-6, through 64 gated of 2816 x 2048: 336 / 355 / 402.
 int tile_of(int64_t pairs, int32_t n_experts, int32_t n_held, int32_t n_rows, int32_t n_cols, bool shared) {
   const int64_t blocks = (n_rows + 4 * kWaves * kTileRows - 1) / (4 * kWaves * kTileRows);
   const double here = static_cast<double>(pairs) * n_held / n_experts;  // on average
@@ -1033,10 +1035,11 @@ int tile_of(int64_t pairs, int32_t n_experts, int32_t n_held, int32_t n_rows, in
 }
 
 // Few pairs, whose tokens' levels find room in LDS: one launch, as long as the tokens of a matrix, which are rounded one after another, are few
-// too, and, summed, few tokens read the same weights.  One / two launches in us: gated, 6 of 64 experts of 2816 x 2048: 10.5 / 13.2 at one
-// token, 34 / 38 at 8; 2 of 8 of 4096 x 2048: 9.8 / 13.0, 16.5 / 21.7 at 8, 21.8 / 19.0 at 16; one of 4096 x 4096: 9.0 / 12.1, 11.3 / 12.1 at 4,
-// 13.7 / 12.3 at 6; summed, 8 of 256 of 4096 x 1024: 9.7 / 16.1, 49 / 50 at 8; 2 of 8 of 4096 x 2048: 17 / 21 at 4, 23 / 22 at 6.  Rows of levels are 16 bytes further apart than they are long, so that
-// the same column of neighbours lies in different banks.
+// too, and, summed, few tokens read the same weights.  One launch / two or three, calls in a row from Python, in us: gated, 6 of 64 experts of
+// 2816 x 2048: 10.1 / 13.9 at one token, 33 / 39 at 8; 2 of 8 of 4096 x 2048: 10.1 / 13.6, 17.3 / 21.9 at 8, 23.2 / 19.5 at 16; one of 4096 x 4096:
+// 9.5 / 13.1, 11.6 / 13.0 at 4, 13.8 / 13.1 at 6; summed, 8 of 256 of 4096 x 1024: 10.8 / 17.5, 48 / 51 at 8; 2 of 8 of 4096 x 2048: 15.9 / 19.5 at 4,
+// 22.5 / 20.0 at 6.  Replayed from a graph, where launches cost less, the same but for one of 4096 x 4096 at 4 tokens: 11.5 / 9.7.  Rows of
+// levels are 16 bytes further apart than they are long, so that the same column of neighbours lies in different banks.
 struct Few {
   bool is;
   int stride;

@@ -8,10 +8,10 @@
 // logits and biases are equal; and rows with more large values than the list holds.  Kept apart from the loop, so that neither its registers nor its
 // time suffer (in the loop: 58 layers of 8155 rows of 256 in 32 bits, biased sigmoid scores, top-8 in four of eight groups, 261 us against
 // 232 at that time).
-// Those rows now: 186 us, 2.8 TB/s read, where all in 64 bits took 717; with sums and 4077 rows 136 us.  Bound by instruction issue (1235
+// Those rows now: 190 us, 2.7 TB/s, where all in 64 bits took 717; with sums and 4077 rows 137 us.  Bound by instruction issue (1237
 // vector instructions per eight rows, a fifth of them for the sigmoids, half of whose time is exp and reciprocal) and by waits for LDS: three
-// waves a SIMD, by registers (168) and LDS (50 KB).  With sums of biased scores ten registers spill, which costs less than the third
-// wave gives (136 against 185).
+// waves a SIMD, by registers (168) and LDS (50 KB).  With sums of biased scores fourteen registers spill, which costs less than the third
+// wave gives (137 against 185).
 #include "route_kernels.h"
 
 namespace tacg {
